@@ -74,6 +74,10 @@ asd_status asd8_kv_quantize(const asd_dims* dims, const void* k_cache, const voi
  * asd_tree_attention with the context in an 8-bit cache:
  *   K_j = k[j] * 2^e of its block, V_j likewise; tree_k, tree_v, q, out bf16.
  * A NaN or an infinity in tree_k or tree_v reaches only the rows that attend to its node.
+ * What is rounded, beside the output: a softmax weight by 2^-8 of it or, in the context, by
+ * 2^-16 of the largest product of a weight and a V scale among the 32 positions [32 i, 32 i +
+ * 32) it is in, where that is more.  So neither tokens far below the row's largest weight
+ * nor blocks of V far below the largest lose what they add.
  * With one node per sequence (max_nodes 1, parent -1) it is the attention of a plain
  * decode step.
  */

@@ -8,34 +8,42 @@
 //                  bf16 MMA's time, products exact, fp32 sums
 //   x_j            = S_j log2(e)/sqrt(D) 2^(eq + ek[block of j]): the block scales of K
 //                  are factors of the exponent
-//   P_j            = 2^(x_j - m) 2^(ev[block of j] - E), E the largest ev so far, again in
-//                  two e4m3 terms (2^-8 of P, 2^-16 of the row's largest at least):
-//                  the block scales of V are factors of the weights
-//   O += P V       two MMAs over e4m3 V, output O 2^E / sum_j 2^(x_j - m)
+//   P_j            = 2^(x_j + ev[block of j] - G + 7), ev the exponents of V's blocks, G the
+//                  largest floor(x_j + ev) among the 32 keys that an MMA step takes: at most
+//                  2^8, again in two e4m3 terms (2^-8 of P, 2^-16 of the group's largest at
+//                  least)
+//   O += 2^(G-7-R) P V   two block-scaled MMAs over e4m3 V: the power of two is the MMA's scale
+//                  byte of the row and the group, so no weight is small in its own group, however
+//                  far the group's lie below the row's largest or its V below the largest V;
+//                  output O 2^R / sum_j 2^x_j
+//
+// (With one reference for all of a row's weights, e4m3's smallest step was 2^-15 of it.  What
+// lay below half of that was lost to P.V and not to the sum: a token with 0.9 of the weight
+// in front of 16384 others cost them a quarter of what they add.)
+//
+// R, an integer per row, keeps O within fp32: it is moved, and O rescaled, when a group's G
+// exceeds it by more than kSlack, which scores of a model hardly ever do after their first
+// tile.
 //
 // The last key tile holds the tree's own K and V in bf16: S and P.V of that tile are
-// kind::f16 MMAs on a bf16 copy of q and on P 2^-E in bf16.
+// kind::f16 MMAs on a bf16 copy of q and on P = 2^(x - R) <= 2 in bf16 (2^-8 of each weight).
 //
 // Work items, chunks and their merge are those of attention_tc.cu's one-tile form.  Where
-// items have at most 64 (32) query rows, TMEM holds two (four) copies of them, and the
-// copies take the key tiles in turn, each with its own maxima, sums and O: a copy's softmax
-// has two (four) tiles' time, and P is 0 in the other copies' lanes.  The reference max m
-// is kept within 2^2.75 of the running one and P scaled by 2^6, so that P <= 448 and its
-// small values stay far from e4m3's subnormals.  On scores as spread as a model's, some row
-// of a warp moves its m in every few tiles; O is rescaled behind the weights, which leaves
-// P.V of the tile before their time to finish, and all rows of the warp move at once (8 x 64
-// nodes at context 16384 188 -> 167 us, 32 adaptive trees 103 -> 84).
+// items have few query rows, TMEM holds copies of them (up to 64 rows two; up to 32 three, four
+// with D = 64), and the copies take the key tiles in turn, each with its own maxima, sums and
+// O: a copy's softmax has that many tiles' time, and P is 0 in the other copies' lanes.  S of a
+// tile is written to its copy's lanes only, so that the copies' S share their columns.
 //
 // More rows fill the tile, and the softmax is what takes the time.  The two threads of a lane
 // then have an O each, the P.V of the tile's first and second 64 keys, and neither waits for
 // the other within a tile; the output joins them as it does copies (8 x 64 nodes at context
 // 16384 175 -> 168 us).
 //
-// TMEM (512 columns): O [0, D); one copy or two: S [128, 256), [256, 384), P [384, 448),
-// [448, 512); four: S [128, 256), P of copy k [256 + 64 k, 320 + 64 k).  S is free for the
-// next tile as soon as its softmax has it in registers.  An O for either key half: O [0, 2 D);
-// with D = 128 S [256, 384), [384, 512), and each thread's P over its 64 columns of S, which
-// are free for the tile after next when P.V is done.
+// TMEM (512 columns): with copies O [0, D), S [128, 256), P of copy k [256 + 64 k, 320 + 64 k),
+// scales [448, 512) with D = 128 (which leaves room for three copies), [64, 128) with D = 64.
+// An O for either key half: O [0, 2 D), then two (D = 64: three) buffers of 128 columns for S;
+// each thread's P stands over its 64 columns of S and the tile's scales behind the first
+// thread's P, all free when P.V is done.
 //
 // Warp roles (384 threads): warps 0 and 3 copy the even and the odd key tiles, K and V, and
 // their block scales, warp 1 issues the S MMAs, warp 2 allocates TMEM and issues the P.V
@@ -70,8 +78,9 @@ constexpr int kCols = kKeys / kSplit;         // keys of a tile that a thread ta
 constexpr int kSoftmax8 = 128 * kSplit;
 constexpr int kThreads8 = 128 + kSoftmax8;
 constexpr int kRing = 4;          // barriers of S, P and P.V, in turn
-constexpr float kBias = 6.f;            // P is 2^(x - m + kBias)
-constexpr float kRescale = 2.75f;       // and m is moved when x - m exceeds this
+constexpr int kGroup = 32;        // keys of an MMA step, under one scale byte of a row
+constexpr float kTop = 7.f;       // a group's largest weight is held in [2^7, 2^8]
+constexpr float kSlack = 32.f;    // R is moved when a group's G exceeds it by more
 
 // Dynamic shared memory, 1024-byte aligned: q1, q2 [128 rows][D bytes], q in bf16
 // [D/64][128 rows][128 bytes], the K ring, the V ring.  The tree's bf16 K and V tiles
@@ -106,14 +115,12 @@ __device__ __forceinline__ int swz8(int r, int c) {
   return r * D + ((D == 128 ? c ^ (r & 7) : c ^ ((r >> 1) & 3)) << 4);
 }
 
-// kind::f8f6f4 instruction descriptor: e4m3 x e4m3 -> fp32; B K-major or MN-major.
-__device__ __forceinline__ uint32_t idesc_f8(int m, int n, bool b_mn) {
-  return (1u << 4) | (b_mn ? (1u << 16) : 0u) | (static_cast<uint32_t>(n >> 3) << 17) |
-         (static_cast<uint32_t>(m >> 4) << 24);
+// kind::f8f6f4 instruction descriptor: e4m3 x e4m3 -> fp32, both K-major.
+__device__ __forceinline__ uint32_t idesc_f8(int m, int n) {
+  return (1u << 4) | (static_cast<uint32_t>(n >> 3) << 17) | (static_cast<uint32_t>(m >> 4) << 24);
 }
 
-// MMAs and commits that the issuing warp runs converged, with `on` set in one lane (see
-// lmhead_fp8.cu).
+// MMAs that the issuing warp runs converged, with `on` set in one lane (tc.cuh).
 #define ASD_MMA_ON(name, kind, atype, aop, acon)                                              \
   __device__ __forceinline__ void name(uint32_t d, atype a, uint64_t b, uint32_t idesc,       \
                                        uint32_t accumulate, uint32_t on) {                    \
@@ -126,17 +133,38 @@ __device__ __forceinline__ uint32_t idesc_f8(int m, int n, bool b_mn) {
         : "memory");                                                                          \
   }
 ASD_MMA_ON(mma_f8, "f8f6f4", uint64_t, "%1", "l")
-ASD_MMA_ON(mma_f8_ts, "f8f6f4", uint32_t, "[%1]", "r")
 ASD_MMA_ON(mma_bf16, "f16", uint64_t, "%1", "l")
 ASD_MMA_ON(mma_bf16_ts, "f16", uint32_t, "[%1]", "r")
 #undef ASD_MMA_ON
-__device__ __forceinline__ void commit_on(uint64_t* bar, uint32_t on) {
+// The same, leaving D as it is in the lanes of quarter k where `skip[k]` is all ones.
+#define ASD_MMA_LANES_ON(name, kind)                                                          \
+  __device__ __forceinline__ void name(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc,    \
+                                       const uint32_t (&skip)[4], uint32_t accumulate,        \
+                                       uint32_t on) {                                         \
+    asm volatile(                                                                             \
+        "{\n\t.reg .pred p, q;\n\t"                                                           \
+        "setp.ne.b32 p, %4, 0;\n\t"                                                           \
+        "setp.ne.b32 q, %5, 0;\n\t"                                                           \
+        "@q tcgen05.mma.cta_group::1.kind::" kind                                             \
+        " [%0], %1, %2, %3, {%6, %7, %8, %9}, p;\n\t}" ::"r"(d),                              \
+        "l"(a), "l"(b), "r"(idesc), "r"(accumulate), "r"(on), "r"(skip[0]), "r"(skip[1]),     \
+        "r"(skip[2]), "r"(skip[3])                                                            \
+        : "memory");                                                                          \
+  }
+ASD_MMA_LANES_ON(mma_f8_lanes, "f8f6f4")
+ASD_MMA_LANES_ON(mma_bf16_lanes, "f16")
+#undef ASD_MMA_LANES_ON
+// A (TMEM) x B with a scale byte per row and 32 columns of A, and of B.
+__device__ __forceinline__ void mma_mx8_ts(uint32_t d, uint32_t a, uint64_t b, uint32_t idesc,
+                                           uint32_t sfa, uint32_t sfb, uint32_t accumulate,
+                                           uint32_t on) {
   asm volatile(
-      "{\n\t.reg .pred q;\n\t"
-      "setp.ne.b32 q, %1, 0;\n\t"
-      "@q tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];\n\t}" ::"r"(
-          smem_u32(bar)),
-      "r"(on)
+      "{\n\t.reg .pred p, q;\n\t"
+      "setp.ne.b32 p, %4, 0;\n\t"
+      "setp.ne.b32 q, %7, 0;\n\t"
+      "@q tcgen05.mma.cta_group::1.kind::mxf8f6f4.block_scale.scale_vec::1X [%0], [%1], %2, %3, "
+      "[%5], [%6], p;\n\t}" ::"r"(d),
+      "r"(a), "l"(b), "r"(idesc), "r"(accumulate), "r"(sfa), "r"(sfb), "r"(on)
       : "memory");
 }
 // ------------------------------------------------------------------- producers
@@ -203,73 +231,53 @@ __device__ __forceinline__ void issue_tile(int row, int br, uint32_t dst, uint32
 // ---------------------------------------------------------------- block scales
 // Factors of context tile t for every 8 of its keys, in a ring of kScaleSlots tiles;
 // they are written once the tile's K slot was free.  (Then the ring's slot is: S of
-// tile t - 4 was done, so the copies had read S up to tile t - 5 at least, and each had
-// finished its tile before, t - 9 or later.)
+// tile t - 4 was issued, so the copies had read S up to tile t - 8 at least, and each had
+// finished its tile before, t - 12 or later.)
 constexpr int kScaleSlots = 16;
 constexpr int kGroups = kKeys / 8;
-constexpr int kNoBlock = -1000;   // no key of the context, or a page outside the pool
 struct TileScales {
   float fk[kGroups];   // 2^ek
-  float gd[kGroups];   // d = ev - E, at least -64 (a weight times 2^-64 is 0 in e4m3); of the
-                       // tree tile -E: the weights are computed times 2^d
-  float gi[kGroups];   // 2^-d, for the row sum
-  int E;               // the weights of this tile are for O in units of 2^E
+  float ev[kGroups];   // ev
+  float gi[kGroups];   // 2^-ev, for the row sum
 };
 
-// 2^e, 0 below the normal numbers.
-__device__ __forceinline__ float pow2_flush(int e) { return e < -126 ? 0.f : pow2(min(e, 127)); }
-
 // A producer writes them behind its tile's copy: lane j < 16 K's byte for keys [8 j,
-// 8 j + 8), lane 16 + j V's.  For E, the largest scale of V up to the tile, it looks at the
-// bytes of the other producer's tiles too.
+// 8 j + 8), lane 16 + j V's.
 struct Scales {
   const Attn8Params& p8;
   const Item& it;
   Pages& pages;
   const uint8_t* exps;   // of this lane's tensor and KV head (paged: page 0's)
-  const uint8_t* v_exps;
-  int bsh, lane, E = kNoBlock;
+  int bsh, lane;
   __device__ __forceinline__ Scales(const Attn8Params& p, const Item& i, Pages& pg)
       : p8(p), it(i), pages(pg), lane(threadIdx.x & 31) {
     bsh = 31 - __clz(p8.block);
-    const size_t at = (static_cast<size_t>(p8.a.page_size ? 0 : it.b) * p8.a.Hkv + it.g) * p8.blocks;
-    exps = (lane < 16 ? p8.k_exp : p8.v_exp) + at;
-    v_exps = p8.v_exp + at;
+    exps = (lane < 16 ? p8.k_exp : p8.v_exp) +
+           (static_cast<size_t>(p8.a.page_size ? 0 : it.b) * p8.a.Hkv + it.g) * p8.blocks;
   }
-  // The byte of the lane's keys of tile t, and (lanes below 16) V's of tile t - 1; -1 past
-  // the context.  Nothing is done with what is loaded, so that it can stay on its way.
-  __device__ __forceinline__ int2 fetch(int t) {
-    if (t <= it.nctx) pages.stage(it.key_base + t * kKeys, lane);
-    const size_t a = at(t), b = lane < 16 ? at(t - 1) : kNone;
-    int2 v = make_int2(-1, -1);
-    if (a != kNone) v.x = exps[a];
-    if (b != kNone) v.y = v_exps[b];
-    return v;
-  }
-  static constexpr size_t kNone = ~static_cast<size_t>(0);
-  __device__ __forceinline__ size_t at(int t) const {
+  // The byte of the lane's keys of tile t; the smallest scale's past the context and in pages
+  // outside the pool.  Nothing is done with what is loaded, so that it can stay on its way.
+  __device__ __forceinline__ int fetch(int t) {
+    constexpr int kNone = kMinExp + kExpBias;
+    if (t >= it.nctx) return kNone;
+    pages.stage(it.key_base + t * kKeys, lane);
     const int k = t * kKeys + 8 * (lane & 15);
-    if (t < 0 || t >= it.nctx || k >= it.ctx) return kNone;
+    if (k >= it.ctx) return kNone;
     const int key = it.key_base + k;
-    if (p8.a.page_size == 0) return static_cast<size_t>(key >> bsh);
+    if (p8.a.page_size == 0) return exps[key >> bsh];
     const int g = pages.page(key);
     return g < 0 ? kNone
-                 : static_cast<size_t>(g) * p8.a.Hkv * p8.blocks + ((key & (p8.a.page_size - 1)) >> bsh);
+                 : exps[static_cast<size_t>(g) * p8.a.Hkv * p8.blocks + ((key & (p8.a.page_size - 1)) >> bsh)];
   }
-  // Tile t's factors from its bytes.
-  __device__ __forceinline__ void write(bool tree, int2 bytes, TileScales& s) {
-    const int e = bytes.x < 0 ? kNoBlock : bytes.x - kExpBias;
-    const int before = bytes.y < 0 ? kNoBlock : bytes.y - kExpBias;
-    E = max(E, __reduce_max_sync(0xffffffffu, max(lane >= 16 ? e : kNoBlock, before)));
-    if (tree && E == kNoBlock) E = 0;
+  // A tile's factors from its bytes.
+  __device__ __forceinline__ void write(int byte, TileScales& s) {
+    const int e = min(max(byte - kExpBias, kMinExp), 126);
     if (lane < 16) {
-      s.fk[lane] = pow2_flush(max(e, kMinExp));
+      s.fk[lane] = pow2(e);
     } else {
-      const int d = tree ? -E : (e == kNoBlock ? 0 : max(e - E, -64));
-      s.gd[lane - 16] = static_cast<float>(d);
-      s.gi[lane - 16] = pow2(-d);
+      s.ev[lane - 16] = static_cast<float>(e);
+      s.gi[lane - 16] = pow2(-e);
     }
-    if (lane == 0) s.E = E;
     __syncwarp();
   }
 };
@@ -311,9 +319,9 @@ __device__ __forceinline__ uint4 only_finite(uint4 v) {
 
 struct Shared {   // what the roles share, beside the tiles
   uint64_t k_full[kStages], k_empty[kStages], v_full[kStages], v_empty[kStages];
-  // tile t's are those of index t % kRing (s_empty: t % S buffers)
+  // tile t's are those of index t % kRing (s_empty: t % copies)
   uint64_t s_full[kRing];    // S in TMEM (MMA -> softmax)
-  uint64_t s_empty[2];       // S in registers (softmax -> MMA)
+  uint64_t s_empty[4];       // S of a copy in registers (softmax -> MMA)
   uint64_t p_full[kRing];    // P in TMEM (softmax -> MMA)
   uint64_t pv_done[kRing];   // O += P V done (MMA -> softmax)
   uint64_t q_ready, mma_done[2];
@@ -322,9 +330,12 @@ struct Shared {   // what the roles share, beside the tiles
   uint64_t tree_clean;       // V's rows of no node, and values that are not finite, are 0
   uint64_t anc[kMaxNodes][2];
   TileScales sc[kScaleSlots];
+  // scale bytes of the tiles' P (index t % kRing) as tc_copy_scales takes them, and V's, 2^0
+  __align__(16) uint32_t sfa[kRing][kRows];
+  __align__(16) uint32_t sfb[kRows];
   float mx[2][kSplit][kRows]; // [parity][key half][TMEM lane]: partial row max
   float l[kSplit][kRows];     // partial row sum
-  float m[kRows];
+  float m[kRows], unit[kRows];
   uint32_t tmem;
   int odd_v;                 // the tree's V rows hold values that are not finite
   int abort;
@@ -338,25 +349,36 @@ struct Shared {   // what the roles share, beside the tiles
 // that the code knows is worth 5 to 10 %; code for several numbers in one kernel costs calls
 // that mix them more (fetched anew by every CTA of another number: ragged trees of 64 columns
 // 52 -> 72 us).  So the host chooses (kernel_of_rows).
+constexpr int kManyCopies = 4;   // REP: as many as TMEM has room for
 template <int D, int REP>
 struct Copies {
-  int own;   // 1, 2 or 4
+  static constexpr int kMost = D == 64 ? 4 : 3;
+  int own;   // 1, 2 or kMost
   __device__ __forceinline__ explicit Copies(int nrows)
-      : own(__all_sync(0xffffffffu, nrows <= 32) ? 4 : (__all_sync(0xffffffffu, nrows <= 64) ? 2 : 1)) {}
-  __device__ __forceinline__ int rep() const { return REP > 0 ? REP : own; }
-  __device__ __forceinline__ int s_bufs() const { return rep() == 4 ? 1 : 2; }
-  __device__ __forceinline__ int p_bufs() const { return rep() == 4 ? 4 : 2; }
-  __device__ __forceinline__ int warps() const { return kSoftmax8 / 32 / rep(); }   // of a copy
-  // each key half has an O of its own, the second at column D; of 128 columns P then takes the
-  // place of S
-  static constexpr bool kHalves = REP == 1, kOver = kHalves && D == 128;
+      : own(__all_sync(0xffffffffu, nrows <= 32) ? kMost : (__all_sync(0xffffffffu, nrows <= 64) ? 2 : 1)) {}
+  __device__ __forceinline__ int rep() const { return REP == 0 ? own : (REP == kManyCopies ? kMost : REP); }
+  __device__ __forceinline__ int span() const {   // TMEM lanes of a copy
+    return rep() > 2 ? kRows / 4 : kRows / rep();
+  }
+  __device__ __forceinline__ int warps() const { return span() / 32 * kSplit; }   // softmax, of a copy
+  // Each key half has an O of its own, the second at column D; P then takes the place of S,
+  // in kOverBufs buffers.
+  static constexpr bool kHalves = REP == 1;
+  static constexpr int kOverBufs = D == 64 ? 3 : 2;
+  __device__ __forceinline__ int p_bufs() const { return kHalves ? kOverBufs : max(rep(), 2); }
   __device__ __forceinline__ uint32_t s_col(int t) const {
-    return rep() == 4 ? 128 : (kOver ? 256 : 128) + 128 * (t & 1);
+    return kHalves ? 2 * D + 128 * (t % kOverBufs) : 128;
   }
   __device__ __forceinline__ uint32_t p_col(int t) const {
-    return rep() == 4 ? 256 + 64 * (t & 3) : 384 + 64 * (t & 1);
+    return kHalves ? s_col(t) : 256 + 64 * (t % p_bufs());
   }
-  __device__ __forceinline__ int s_use(int t) const { return rep() == 4 ? t : t >> 1; }
+  // scale words of P and of V
+  __device__ __forceinline__ uint32_t sfa_col(int t) const {
+    return kHalves ? s_col(t) + kCols / 2 : sfb_col(t) + 4 + 4 * (t % p_bufs());
+  }
+  __device__ __forceinline__ uint32_t sfb_col(int t) const {
+    return kHalves ? s_col(t) + kCols / 2 + 4 : (D == 64 ? 64 : 448);
+  }
 };
 
 // AND of `v` over the softmax warps of a TMEM lane quarter; uniform result.
@@ -387,8 +409,8 @@ struct Softmax {
   float c_row;
   uint64_t anc;              // the row's ancestors among the thread's keys of the tree tile
   long long budget;
-  float m_ref, l;
-  int E;
+  float R;                   // O is in units of 2^R; -infinity before the row's first key
+  float m, l;                // sum of the weights 2^(x - m), m an integer
 
   __device__ __forceinline__ void mask(float (&x)[kCols], bool tree, int valid) const {
     const int own = min(max(valid - kCols * cq, 0), kCols);
@@ -398,31 +420,50 @@ struct Softmax {
 #pragma unroll
     for (int k = 0; k < kCols; ++k) x[k] = (w[k >> 5] >> (k & 31)) & 1u ? x[k] : -INFINITY;
   }
-  __device__ __forceinline__ float maximum(const float (&x)[kCols], const TileScales& sc, bool tree) const {
-    const float* fk = sc.fk + cq * (kCols / 8);
+  // The largest x, and the largest x + ev of either group of keys (of the tree tile x).
+  __device__ __forceinline__ float maximum(const float (&x)[kCols], const TileScales& sc, bool tree,
+                                           float (&u)[kCols / kGroup]) const {
+    const int s0 = cq * (kCols / 8);
     float mt = -INFINITY;
 #pragma unroll
-    for (int g = 0; g < kCols / BLK; ++g) {
-      float mg = fmaxf(x[BLK * g], x[BLK * g + 1]);
+    for (int h = 0; h < kCols / kGroup; ++h) {
+      u[h] = -INFINITY;
 #pragma unroll
-      for (int k = 2; k < BLK; k += 2) mg = fmaxf(fmaxf(mg, x[BLK * g + k]), x[BLK * g + k + 1]);
-      mt = fmaxf(mt, mg * (tree ? p8.a.scale_log2 : c_row * fk[g * (BLK / 8)]));
+      for (int g = h * kGroup; g < (h + 1) * kGroup; g += BLK) {
+        float mg = fmaxf(x[g], x[g + 1]);
+#pragma unroll
+        for (int k = 2; k < BLK; k += 2) mg = fmaxf(fmaxf(mg, x[g + k]), x[g + k + 1]);
+        mg *= tree ? p8.a.scale_log2 : c_row * sc.fk[s0 + g / 8];
+        mt = fmaxf(mt, mg);
+        u[h] = fmaxf(u[h], tree ? mg : mg + sc.ev[s0 + g / 8]);
+      }
     }
     return mt;
   }
   // The weights, as P: words of 4 e4m3 of either term (the second `lo_at` columns behind), the
-  // tree tile's as bf16 pairs.  p_at: the thread's keys'.
-  __device__ __forceinline__ void weights(const float (&x)[kCols], uint32_t p_at, uint32_t lo_at,
-                                          const TileScales& sc, bool tree) {
-    const float mu = m_ref == -INFINITY ? 0.f : m_ref - kBias;
+  // groups' scale bytes at `sf`; the tree tile's as bf16 pairs.  p_at: the thread's keys'.
+  // mt, u: from maximum.
+  __device__ __forceinline__ void weights(const float (&x)[kCols], float mt, const float (&u)[kCols / kGroup],
+                                          uint32_t p_at, uint32_t lo_at, const TileScales& sc,
+                                          uint32_t* sf, bool tree) {
+    const float rz = R == -INFINITY ? 0.f : R, mn = fmaxf(m, floorf(mt)), mz = mn == -INFINITY ? 0.f : mn;
+    l *= ex2_approx(m - mz);   // (0 before the first key, with l)
+    m = mn;
     if (!tree) {
+      uint32_t bytes = 0;
 #pragma unroll
-      for (int h = 0; h < kCols / 32; ++h) {
+      for (int h = 0; h < kCols / kGroup; ++h) {
         uint32_t hi[8], lo[8];
+        // (finite where the group has no key)
+        const float top = fmaxf(floorf(u[h]), -1e6f) - kTop;
+        // 2^(top - R), as little as a scale byte holds where it is less
+        const float b = fminf(fmaxf(top - rz + 127.f, 0.f), 254.f);
+        bytes |= static_cast<uint32_t>(b) << (8 * h);
+        const float to_sum = ex2_approx(top - mz);
 #pragma unroll
-        for (int g = 0; g < 32 / BLK; ++g) {
-          const int at = 32 * h + BLK * g, sg = (cq * kCols + at) / 8;
-          const float f = c_row * sc.fk[sg], nb = sc.gd[sg] - mu;
+        for (int g = 0; g < kGroup / BLK; ++g) {
+          const int at = kGroup * h + BLK * g, sg = (cq * kCols + at) / 8;
+          const float f = c_row * sc.fk[sg], nb = sc.ev[sg] - top;
           const uint64_t f2 = pack_f32x2(f, f), nb2 = pack_f32x2(nb, nb);
           uint64_t sum = 0ull;
 #pragma unroll
@@ -440,28 +481,31 @@ struct Softmax {
           }
           float s0, s1;
           unpack_f32x2(sum, s0, s1);
-          l = fmaf(s0 + s1, sc.gi[sg], l);
+          l = fmaf((s0 + s1) * sc.gi[sg], to_sum, l);
         }
         tmem_st8u(p_at + 8 * h, hi);
         tmem_st8u(p_at + lo_at + 8 * h, lo);
       }
+      reinterpret_cast<uint16_t*>(sf)[((row & 31) * 4 + (row >> 5)) * 2 + cq] = static_cast<uint16_t>(bytes);
+      fence_proxy_async();   // the tensor core's copy reads them
     } else {
-      const float f = p8.a.scale_log2, nb = sc.gd[0] - mu;
+      const float f = p8.a.scale_log2;
       float s = 0.f;
 #pragma unroll
       for (int h = 0; h < kCols / 32; ++h) {
         uint32_t pk[16];
 #pragma unroll
         for (int k = 0; k < 32; k += 2) {
-          const float p0 = ex2_approx(fmaf(x[32 * h + k], f, nb));
-          const float p1 = ex2_approx(fmaf(x[32 * h + k + 1], f, nb));
+          const float p0 = ex2_approx(fmaf(x[32 * h + k], f, -rz));
+          const float p1 = ex2_approx(fmaf(x[32 * h + k + 1], f, -rz));
           s += p0 + p1;
           __nv_bfloat162 v = __floats2bfloat162_rn(p0, p1);
           pk[k / 2] = *reinterpret_cast<uint32_t*>(&v);
         }
         tmem_st16u(p_at + 16 * h, pk);
       }
-      l = fmaf(s, sc.gi[0], l);
+      // (beyond 2^126 nothing of s is left: this thread's keys are as far below the row's)
+      l = fmaf(s, ex2_approx(fminf(rz - mz, 126.f)), l);
     }
   }
   // O += P V of tile t is done.  (The caller knows that tile t - 4's is, and that tile
@@ -472,36 +516,37 @@ struct Softmax {
 
   // Every tile of the copy; false when a bounded wait gave up.
   // HALVES: the two threads of a lane do not know of each other: their key halves have
-  // maxima, sums and an O each, and (OVER) P is written over the half's S.
+  // maxima, sums and an O each, and P is written over the half's S.
   __device__ __forceinline__ bool run() {
-    constexpr bool HALVES = Copies<D, REP>::kHalves, OVER = Copies<D, REP>::kOver;
+    constexpr bool HALVES = Copies<D, REP>::kHalves;
     using G = Geom<D>;
     const int quarter = warp_index() & 3, lane = threadIdx.x & 31;
     bool bad = false;
     int e = 0;
-    m_ref = -INFINITY;
+    R = m = -INFINITY;
     l = 0.f;
-    E = kNoBlock;
+    if (copy >= cp.rep()) return true;   // lanes of no copy
     for (int t = copy; t < it.ntiles; t += cp.rep(), e ^= 1) {
       const bool tree = t >= it.nctx;
       const int valid = tree ? it.n : min(kKeys, it.ctx - t * kKeys);
       const TileScales& sc = sh.sc[t % kScaleSlots];
       const bool here = !bad && wait_warp(&sh.s_full[t % kRing], (t / kRing) & 1, budget);
-      float x[kCols], mt = -INFINITY;
+      float x[kCols], mt = -INFINITY, u[kCols / kGroup], top = -INFINITY;
       if (here) {
         if (busy) {
           tc_fence_after();
           tmem_ld64(lane_base + cp.s_col(t) + kCols * cq, x);
           tc_fence_before();
         }
-        if (!OVER) {
+        if (!HALVES) {
           __syncwarp();
-          if (lane == 0) mbar_arrive(smem_u32(&sh.s_empty[t & (cp.s_bufs() - 1)]));
+          if (lane == 0) mbar_arrive(smem_u32(&sh.s_empty[copy]));
         }
         if (busy) {
           if (tree || valid < kKeys) mask(x, tree, valid);
-          mt = maximum(x, sc, tree);
-          if (!HALVES) sh.mx[e][cq][row] = mt;
+          mt = maximum(x, sc, tree, u);
+          top = floorf(fmaxf(u[0], u[1]));
+          if (!HALVES) sh.mx[e][cq][row] = top;
         }
       }
       if (HALVES) {
@@ -509,30 +554,19 @@ struct Softmax {
       } else {
         // the quarter's warps decide together whether to go on, and the maxima become visible
         if (!quarter_all(quarter, here)) return false;
-        mt = fmaxf(sh.mx[e][0][row], sh.mx[e][1][row]);
+        top = fmaxf(sh.mx[e][0][row], sh.mx[e][1][row]);
       }
-      // P's columns are free (OVER: S of tile t came behind P.V of tile t - 2)
-      if (!OVER && t >= cp.p_bufs() && !wait_pv(t - cp.p_bufs())) bad = true;
+      // P's columns are free (HALVES: S of tile t came behind the P.V before)
+      if (!HALVES && t >= cp.p_bufs() && !wait_pv(t - cp.p_bufs())) bad = true;
       if (busy) {
-        const float mn = fmaxf(mt, m_ref);
-        const bool had = m_ref != -INFINITY;
-        bool need = had ? (mn > m_ref + kRescale) : (mn != -INFINITY);
-        const int now = sc.E;
-        const bool rescale = t >= cp.rep() && (__any_sync(0xffffffffu, need && had) || now != E);
-        // where one of the warp's rows moves its reference all do: the next that has to is
-        // then many tiles away (the tree's tile, the last, keeps rows apart)
-        if (rescale) need = need || (!tree && mn > m_ref);
-        const float moved = need && had ? exp2f(m_ref - mn) : 1.f;
-        const float alpha = moved * pow2_flush(E - now);
-        E = now;
-        if (need) {
-          l *= moved;
-          m_ref = mn;
-        }
-        if (OVER)
-          weights(x, lane_base + cp.s_col(t) + kCols * cq, 16, sc, tree);
-        else
-          weights(x, lane_base + cp.p_col(t) + cq * (tree ? kCols / 2 : kCols / 4), 32, sc, tree);
+        // (the tree's weights are not scaled: none above 2)
+        const bool had = R != -INFINITY, need = had ? top > R + (tree ? 0.f : kSlack) : top != -INFINITY;
+        const bool rescale = t >= cp.rep() && __any_sync(0xffffffffu, need && had);
+        const float alpha = need && had ? exp2f(R - top) : 1.f;
+        if (need) R = top;
+        const uint32_t p_at = lane_base + cp.p_col(t) +
+                              cq * (HALVES ? kCols : tree ? kCols / 2 : kCols / 4);
+        weights(x, mt, u, p_at, HALVES ? kCols / 4 : kCols / 2, sc, sh.sfa[t % kRing], tree);
         if (rescale) {
           // O holds earlier tiles: rescale this thread's half of the row's columns, or its own
           // O.  (The other copies' P.V adds 0 to them, so it has to be done too.)  P.V of the
@@ -561,7 +595,7 @@ struct Softmax {
         // t - 4, consumed: P.V of tile t - 4 is done.)
         if (!bad && wait_warp(&sh.v_full[t % kStages], (t / kStages) & 1, budget)) {
           // thread among those of the copy
-          const int per = 4 / cp.rep(), tid = (cq * per + (quarter & (per - 1))) * 32 + lane;
+          const int per = cp.span() / 32, tid = (cq * per + (quarter & (per - 1))) * 32 + lane;
           const int of = kSplit * 32 * per;
           uint8_t* vt = gbase + G::kVOff + t % kStages * G::kTile;
           constexpr int kChunks = D / 16;
@@ -639,7 +673,7 @@ __device__ __forceinline__ bool softmax_role8(const Attn8Params& p8, const Item&
   const int row = (warp & 3) * 32 + lane;      // = TMEM lane
   const int tid = threadIdx.x - 32 * kSoftmaxWarp;
   const uint32_t lane_base = tmem + (static_cast<uint32_t>((warp & 3) * 32) << 16);
-  const int span = kRows / rep;                // rows of a copy
+  const int span = cp.span();                  // rows of a copy
   const int r = row & (span - 1), copy = row / span;
   const bool mine = r < it.nrows;
   const bool busy = (((warp & 3) * 32) & (span - 1)) < it.nrows;
@@ -696,7 +730,7 @@ __device__ __forceinline__ bool softmax_role8(const Attn8Params& p8, const Item&
     uint32_t z[16];
 #pragma unroll
     for (int i = 0; i < 16; ++i) z[i] = 0u;
-    for (int k = 0; k < rep; ++k)
+    for (int k = 0; rep > 1 && k < rep; ++k)
       if (k != copy)
         for (int c = 0; c < 64 / kSplit; c += 16)
           tmem_st16u(lane_base + cp.p_col(k) + (64 / kSplit) * cq + c, z);
@@ -712,9 +746,8 @@ __device__ __forceinline__ bool softmax_role8(const Attn8Params& p8, const Item&
     tree_masks<kSoftmax8>(p, it, tid, sh.par, sh.anc);
     if (mine) anc = sh.anc[(it.r0 + r) / p.G][cq];
   }
-  Softmax<D, BLK, REP> sm{p8, it, sh, cp, gbase, lane_base, cq, row, copy, busy, c_row, anc, budget, 0.f, 0.f, 0};
+  Softmax<D, BLK, REP> sm{p8, it, sh, cp, gbase, lane_base, cq, row, copy, busy, c_row, anc, budget, 0.f, 0.f, 0.f};
   bool ok = sm.run();
-  const float m_ref = sm.m_ref, l = sm.l;
   // O is complete once every P.V is done
   if (ok) {
     ok = wait_warp(&sh.mma_done[1], 0, budget) && !aborted_warp(&sh.abort) &&
@@ -728,17 +761,21 @@ __device__ __forceinline__ bool softmax_role8(const Attn8Params& p8, const Item&
     }
     return false;
   }
-  sh.l[cq][row] = l;
-  sh.mx[0][cq][row] = m_ref;   // (of the copies' two threads the same)
+  sh.l[cq][row] = sm.l;
+  sh.mx[0][cq][row] = sm.m;
+  sh.mx[1][cq][row] = sm.R;   // (of the copies' two threads the same)
   softmax_sync<kSoftmax8>();
-  // O 2^(m - M) of every copy -> shared memory [128][D + 4] (the tiles are free), all in
-  // units of the last tile's 2^E
-  const int E_last = sh.sc[(it.ntiles - 1) % kScaleSlots].E;
-  float M = fmaxf(sh.mx[0][0][row], sh.mx[0][1][row]);
-  for (int k = 0; k < rep; ++k) M = fmaxf(M, sh.mx[0][0][k * span + r]);
-  const float unit_w = pow2_flush(sm.E - E_last);
-  auto weight = [&](float m) { return m == -INFINITY ? 0.f : exp2f(m - M) * unit_w; };
-  const float w = weight(cp.kHalves ? sh.mx[0][0][row] : m_ref), w1 = weight(sh.mx[0][1][row]);
+  // O of every copy -> shared memory [128][D + 4] (the tiles are free), all in units of the
+  // row's largest 2^R
+  float R = -INFINITY, M = -INFINITY;
+  for (int k = 0; k < rep; ++k)
+#pragma unroll
+    for (int h = 0; h < kSplit; ++h) {
+      M = fmaxf(M, sh.mx[0][h][k * span + r]);
+      R = fmaxf(R, sh.mx[1][h][k * span + r]);
+    }
+  auto weight = [&](float x) { return x == -INFINITY ? 0.f : exp2f(x - R); };
+  const float w = weight(cp.kHalves ? sh.mx[1][0][row] : sm.R), w1 = weight(sh.mx[1][1][row]);
   float* stage = reinterpret_cast<float*>(gbase) + row * (D + 4) + cq * (D / kSplit);
 #pragma unroll
   for (int cc = 0; cc < D / kSplit / 16; ++cc) {
@@ -771,11 +808,11 @@ __device__ __forceinline__ bool softmax_role8(const Attn8Params& p8, const Item&
   if (first) {
     sh.l[0][r] = lt;
     sh.m[r] = M;
+    sh.unit[r] = R == -INFINITY ? 0.f : exp2f(R - M);
   }
   softmax_sync<kSoftmax8>();
   // the copies' sum: the output, or (one of several chunks) the fp32 partial that the
   // merge combines
-  const float unit = pow2(E_last);
   const size_t part = static_cast<size_t>(it.part0) +
                       static_cast<size_t>(it.g * it.chunks + it.chunk) * it.R + it.r0;
   if (it.chunks > 1 && tid < it.nrows) p.part_ml[part + tid] = make_float2(sh.m[tid], sh.l[0][tid]);
@@ -793,6 +830,7 @@ __device__ __forceinline__ bool softmax_role8(const Attn8Params& p8, const Item&
       o[4] += y.x; o[5] += y.y; o[6] += y.z; o[7] += y.w;
     }
     if (sh.odd_v) add_odd(p, it, sh, q, c, o);
+    const float unit = sh.unit[q];
     if (it.chunks > 1) {
       float4* dst = reinterpret_cast<float4*>(p.part_o + (part + q) * D + c);
       dst[0] = make_float4(o[0] * unit, o[1] * unit, o[2] * unit, o[3] * unit);
@@ -860,7 +898,7 @@ __global__ void __launch_bounds__(kThreads8, 1)
     mbar_init(smem_u32(&sh.mma_done[1]), 1);
     sh.abort = sh.tree_issued = sh.odd_v = 0;
     mbar_init(smem_u32(&sh.ctx_done), 1);
-    mbar_init(smem_u32(&sh.tree_k), 2);   // the copy and its scales
+    mbar_init(smem_u32(&sh.tree_k), 1);
     mbar_init(smem_u32(&sh.tree_v), 1);
     mbar_init(smem_u32(&sh.tree_clean), 2);   // either producer's half
     fence_mbar_init();
@@ -883,9 +921,14 @@ __global__ void __launch_bounds__(kThreads8, 1)
   const Copies<D, REP> cp(it.nrows);
   if (threadIdx.x == 32 * 3) {   // the copies' own arrivals
     for (int b = 0; b < kRing; ++b) mbar_init(smem_u32(&sh.p_full[b]), cp.warps());
-    for (int b = 0; b < 2; ++b) mbar_init(smem_u32(&sh.s_empty[b]), cp.warps());
+    for (int b = 0; b < 4; ++b) mbar_init(smem_u32(&sh.s_empty[b]), cp.warps());
     fence_mbar_init();
   }
+  // scale bytes of 2^0 (of rows without keys, whose P is 0 or of no use, no NaN)
+  static_assert(sizeof(sh.sfa) == kRing * sizeof(sh.sfb), "");
+  for (int i = threadIdx.x; i < (kRing + 1) * kRows; i += kThreads8)
+    (i < kRows ? sh.sfb[i] : sh.sfa[i / kRows - 1][i % kRows]) = 0x01010101u * kExpBias;
+  fence_proxy_async();   // the tensor core's copy reads them
   __syncthreads();
   bool ok = true;
 
@@ -912,23 +955,23 @@ __global__ void __launch_bounds__(kThreads8, 1)
                     smem_u32(&full[stage]), which ? &tm_v : &tm_k, pol, lane);
       if (lane == 0) ++sh.issued[which][stage];
     };
-    auto factors = [&](int t, int2 e) {
-      scales.write(t >= it.nctx, e, sh.sc[t % kScaleSlots]);
-      if (lane == 0) mbar_arrive(smem_u32(t >= it.nctx ? &sh.tree_k : &sh.k_full[t % kStages]));
+    auto factors = [&](int t, int e) {
+      scales.write(e, sh.sc[t % kScaleSlots]);
+      if (lane == 0) mbar_arrive(smem_u32(&sh.k_full[t % kStages]));
     };
     // the scales of the first two tiles are on their way first (a small loop: code that runs
     // once costs its fetch; 8 nodes at context 32k 27.8 -> 26.3 us)
-    const int2 e0 = scales.fetch(odd), e1 = scales.fetch(odd + 2);
+    const int e0 = scales.fetch(odd), e1 = scales.fetch(odd + 2);
     int nk = odd, nv;   // next tile of K, of V
 #pragma unroll 1
-    for (int2 e = e0; nk < min(it.nctx, kStages); nk += 2, e = e1) {
+    for (int e = e0; nk < min(it.nctx, kStages); nk += 2, e = e1) {
       const int row = pages.row(nk, lane);
       copy(0, nk, row);
       copy(1, nk, row);
       factors(nk, e);
     }
     nv = nk;
-    int2 next = scales.fetch(nk);   // scale bytes of the next tile, fetched a tile ahead
+    int next = scales.fetch(nk);   // scale bytes of the next tile, fetched a tile ahead
     int last = -1;         // cache row of K's last tile
     while (nv < it.nctx) {
       int row = last;
@@ -962,7 +1005,6 @@ __global__ void __launch_bounds__(kThreads8, 1)
         }
         sh.tree_issued = 1;
       }
-      if (ok) factors(it.nctx, next);
     }
     if (ok && it.ntree > 0) {
       ok = wait_warp(&sh.tree_v, 0, budget);
@@ -983,41 +1025,57 @@ __global__ void __launch_bounds__(kThreads8, 1)
     const uint32_t on = lane == 0 ? 1u : 0u;
     const uint32_t tm = __shfl_sync(0xffffffffu, tmem, 0);
     if (warp == 1) {
-      const uint32_t idesc_s = idesc_f8(kRows, kKeys, false), idesc_t = idesc_bf16(kRows, kKeys);
+      const uint32_t idesc_s = idesc_f8(kRows, kKeys), idesc_t = idesc_bf16(kRows, kKeys);
       ok = wait_warp(&sh.q_ready, 0, budget);
       tc_fence_after();
+      int copy = 0;          // of tile t, and the parity of its tiles before
+      uint32_t use = 0;
       for (int t = 0; ok && t < it.ntiles; ++t) {
         const bool tree = t >= it.nctx;
         const int stage = tree ? 0 : t % kStages, b = t % kRing;
         ok = (tree ? wait_warp(&sh.tree_k, 0, budget)
                    : wait_warp(&sh.k_full[stage], (t / kStages) & 1, budget)) &&
-             (cp.kOver ? t < 2 || wait_warp(&sh.pv_done[(t - 2) % kRing], ((t - 2) / kRing) & 1, budget)
-                          : wait_warp(&sh.s_empty[t & (cp.s_bufs() - 1)], (cp.s_use(t) & 1) ^ 1u, budget));
+             (cp.kHalves ? t < cp.kOverBufs || wait_warp(&sh.pv_done[(t - cp.kOverBufs) % kRing],
+                                                         ((t - cp.kOverBufs) / kRing) & 1, budget)
+                         : wait_warp(&sh.s_empty[copy], use ^ 1u, budget));
         if (!ok) break;
         tc_fence_after();
         const uint32_t kst = base + G::kKOff + stage * G::kTile, sb = tm + cp.s_col(t);
+        // the copy's lanes only
+        uint32_t skip[4];
+#pragma unroll
+        for (int k = 0; k < 4; ++k) skip[k] = 32 * k / cp.span() == copy ? 0u : 0xffffffffu;
         if (!tree) {
 #pragma unroll
           for (int term = 0; term < 2; ++term)
 #pragma unroll
-            for (int ks = 0; ks < D / 32; ++ks)
-              mma_f8(sb, desc8<D>(base + term * G::kQ8 + 32 * ks), desc8<D>(kst + 32 * ks), idesc_s,
-                     term + ks > 0 ? 1u : 0u, on);
+            for (int ks = 0; ks < D / 32; ++ks) {
+              const uint64_t a = desc8<D>(base + term * G::kQ8 + 32 * ks), k = desc8<D>(kst + 32 * ks);
+              if (cp.kHalves) mma_f8(sb, a, k, idesc_s, term + ks > 0 ? 1u : 0u, on);
+              else mma_f8_lanes(sb, a, k, idesc_s, skip, term + ks > 0 ? 1u : 0u, on);
+            }
         } else {
 #pragma unroll
           for (int ks = 0; ks < D / 16; ++ks) {
             const int h = ks >> 2, kk = ks & 3;
-            mma_bf16(sb, sw128_desc(base + G::kQbOff + h * (kRows * 128) + 32 * kk),
-                     sw128_desc(kst + h * (kKeys * 128) + 32 * kk), idesc_t, ks > 0 ? 1u : 0u, on);
+            const uint64_t a = sw128_desc(base + G::kQbOff + h * (kRows * 128) + 32 * kk),
+                           k = sw128_desc(kst + h * (kKeys * 128) + 32 * kk);
+            if (cp.kHalves) mma_bf16(sb, a, k, idesc_t, ks > 0 ? 1u : 0u, on);
+            else mma_bf16_lanes(sb, a, k, idesc_t, skip, ks > 0 ? 1u : 0u, on);
           }
         }
-        commit_on(&sh.s_full[b], on);
-        commit_on(t == it.nctx - 1 ? &sh.ctx_done : &sh.k_empty[stage], on);
+        if (++copy == cp.rep()) {
+          copy = 0;
+          use ^= 1u;
+        }
+        tc_commit_on(smem_u32(&sh.s_full[b]), on);
+        tc_commit_on(smem_u32(t == it.nctx - 1 ? &sh.ctx_done : &sh.k_empty[stage]), on);
       }
     } else {
       ok = wait_warp(&sh.q_ready, 0, budget);   // P is 0 where the copies do not write it
       tc_fence_after();
-      const uint32_t idesc_o = idesc_f8(kRows, D, true), idesc_t = idesc_bf16(kRows, D, true);
+      const uint32_t idesc_o = idesc_mx8(kRows, D, true), idesc_t = idesc_bf16(kRows, D, true);
+      if (!cp.kHalves) tc_copy_scales(tm + cp.sfb_col(0), smem_u32(sh.sfb), on);
       for (int j = 0; ok && j < it.ntiles; ++j) {
         const bool tree = j >= it.nctx;
         const int stage = j % kStages, b = j % kRing;
@@ -1031,21 +1089,25 @@ __global__ void __launch_bounds__(kThreads8, 1)
         tc_fence_after();
         const uint32_t vst = base + (tree ? G::kTreeVOff : G::kVOff + stage * G::kTile);
         // P's columns of MMA step kk: in a row, or behind the start of either key half's S
-        const uint32_t pb = tm + (cp.kOver ? cp.s_col(j) : cp.p_col(j));
-        const uint32_t half = cp.kHalves ? 1u : 0u, o1 = half * D, over = cp.kOver ? 1u : 0u;
-        const uint32_t lo = over ? 16 : 32;
+        const uint32_t pb = tm + cp.p_col(j);
+        const uint32_t half = cp.kHalves ? 1u : 0u, o1 = half * D;
+        const uint32_t lo = half ? kCols / 4 : kCols / 2;
         if (!tree) {
-          const uint32_t skip = over * (kCols - kCols / 4);
+          const uint32_t skip = half * (kCols - kCols / 4);
+          const uint32_t sfa = tm + cp.sfa_col(j), sfb = tm + cp.sfb_col(j);
+          tc_copy_scales(sfa, smem_u32(sh.sfa[b]), on);
+          if (half) tc_copy_scales(sfb, smem_u32(sh.sfb), on);
 #pragma unroll
           for (int term = 0; term < 2; ++term)
 #pragma unroll
-            for (int kk = 0; kk < kKeys / 32; ++kk) {
+            for (int kk = 0; kk < kKeys / kGroup; ++kk) {
               const uint32_t h = kk / 2;
-              mma_f8_ts(tm + h * o1, pb + lo * term + 8 * kk + h * skip, desc8<D>(vst + kk * 32 * D), idesc_o,
-                        (j > 0 || term > 0 || kk > (kk == 2 && half ? 2 : 0)) ? 1u : 0u, on);
+              mma_mx8_ts(tm + h * o1, pb + lo * term + 8 * kk + h * skip, desc8<D>(vst + kk * kGroup * D),
+                         idesc_o | sf_byte_a(kk), sfa, sfb,
+                         (j > 0 || term > 0 || kk > (kk == 2 && half ? 2 : 0)) ? 1u : 0u, on);
             }
         } else {
-          const uint32_t skip = over * (kCols - kCols / 2);
+          const uint32_t skip = half * (kCols - kCols / 2);
 #pragma unroll
           for (int kk = 0; kk < kKeys / 16; ++kk) {
             const uint32_t h = kk / 4;
@@ -1053,8 +1115,8 @@ __global__ void __launch_bounds__(kThreads8, 1)
                         idesc_t, (j > 0 || kk > (kk == 4 && half ? 4 : 0)) ? 1u : 0u, on);
           }
         }
-        commit_on(&sh.pv_done[b], on);
-        if (!tree) commit_on(&sh.v_empty[stage], on);
+        tc_commit_on(smem_u32(&sh.pv_done[b]), on);
+        if (!tree) tc_commit_on(smem_u32(&sh.v_empty[stage]), on);
       }
     }
     if (!ok && lane == 0) {
@@ -1104,7 +1166,7 @@ using Kernel = void(const CUtensorMap, const CUtensorMap, const CUtensorMap, con
 // (items' own number 50), 8 x 64 nodes at 16384 147 (170).
 template <int D, int BLK>
 Kernel* kernel_of_rows(int most, double mean) {
-  return most <= 32   ? attn_kv8_kernel<D, BLK, 4>
+  return most <= 32   ? attn_kv8_kernel<D, BLK, kManyCopies>
          : most <= 64 ? attn_kv8_kernel<D, BLK, 2>
          : mean <= 64 ? attn_kv8_kernel<D, BLK, 0>
                       : attn_kv8_kernel<D, BLK, 1>;

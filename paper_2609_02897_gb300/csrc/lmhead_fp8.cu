@@ -173,18 +173,6 @@ struct Lm8Geom {
 };
 constexpr uint32_t kLm8Tmem = 512;
 
-// kind::mxf8f6f4 instruction descriptor: e4m3 x e4m3 -> fp32, both K-major, scale bytes
-// 2^(b - 127), byte 0 of a scale word (sf_byte adds another).
-__device__ __forceinline__ uint32_t idesc_mx8(int m, int n) {
-  return (static_cast<uint32_t>(n >> 3) << 17) | (1u << 23) | (static_cast<uint32_t>(m >> 4) << 24);
-}
-__device__ __forceinline__ uint32_t sf_byte(int i) {
-  return (static_cast<uint32_t>(i) << 29) | (static_cast<uint32_t>(i) << 4);
-}
-// The issuing warp runs these converged, with `on` set in one lane: under a branch on the
-// lane the descriptors cannot stay in uniform registers, and an MMA took 75 cycles to
-// issue, a wait on a completed barrier 180, which made 1600 cycles a k-block against 1220
-// that its 28 KB of W take to arrive.
 __device__ __forceinline__ void tc_mma_mx8(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc,
                                            uint32_t sfa, uint32_t sfb, uint32_t accumulate,
                                            uint32_t on) {
@@ -195,27 +183,6 @@ __device__ __forceinline__ void tc_mma_mx8(uint32_t d, uint64_t a, uint64_t b, u
       "@q tcgen05.mma.cta_group::1.kind::mxf8f6f4.block_scale.scale_vec::1X [%0], %1, %2, %3, "
       "[%5], [%6], p;\n\t}" ::"r"(d),
       "l"(a), "l"(b), "r"(idesc), "r"(accumulate), "r"(sfa), "r"(sfb), "r"(on)
-      : "memory");
-}
-// 32 rows of 16 bytes in shared memory -> 4 TMEM columns of every lane quarter: row r's
-// word j is the scale word of operand row 32 j + r.
-__device__ __forceinline__ void tc_copy_scales(uint32_t tmem, uint32_t saddr, uint32_t on) {
-  uint64_t d = static_cast<uint64_t>((saddr & 0x3FFFFu) >> 4);
-  d |= static_cast<uint64_t>(128 >> 4) << 32;   // 8 rows of 16 bytes follow each other
-  d |= static_cast<uint64_t>(1) << 46;
-  asm volatile(
-      "{\n\t.reg .pred q;\n\t"
-      "setp.ne.b32 q, %2, 0;\n\t"
-      "@q tcgen05.cp.cta_group::1.32x128b.warpx4 [%0], %1;\n\t}" ::"r"(tmem),
-      "l"(d), "r"(on)
-      : "memory");
-}
-__device__ __forceinline__ void tc_commit_on(uint32_t bar, uint32_t on) {
-  asm volatile(
-      "{\n\t.reg .pred q;\n\t"
-      "setp.ne.b32 q, %1, 0;\n\t"
-      "@q tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];\n\t}" ::"r"(bar),
-      "r"(on)
       : "memory");
 }
 template <int NT>
@@ -382,7 +349,7 @@ __global__ void __launch_bounds__(Lm8Geom<NT>::kThreads, 1)
           if (!ok) break;
           tc_fence_after();
           const uint32_t a_s = base + stage * slot + j * a_blk, w_s = base + stage * slot + NT * a_blk;
-          const uint32_t id = idesc | sf_byte(kb & 3);
+          const uint32_t id = idesc | sf_byte_a(kb & 3) | sf_byte_b(kb & 3);
 #pragma unroll
           for (int k = 0; k < 4; ++k)
             tc_mma_mx8(tm + acc * kLm8TileN, sw128_desc(a_s + 32 * k), sw128_desc(w_s + 32 * k), id,

@@ -88,6 +88,42 @@ __device__ __forceinline__ void tc_commit(uint32_t bar) {
       : "memory");
 }
 
+// MMAs, copies and commits that the issuing warp runs converged, with `on` set in one lane:
+// under a branch on the lane the descriptors cannot stay in uniform registers, and an MMA
+// took 75 cycles to issue, a wait on a completed barrier 180 (an 8-bit LM-head k-block 1600
+// cycles against 1220 that its 28 KB of W take to arrive).
+__device__ __forceinline__ void tc_commit_on(uint32_t bar, uint32_t on) {
+  asm volatile(
+      "{\n\t.reg .pred q;\n\t"
+      "setp.ne.b32 q, %1, 0;\n\t"
+      "@q tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];\n\t}" ::"r"(bar),
+      "r"(on)
+      : "memory");
+}
+
+// kind::mxf8f6f4 instruction descriptor: e4m3 x e4m3 -> fp32, A K-major, B K-major or
+// MN-major, scale bytes 2^(b - 127), byte 0 of the scale words (sf_byte_a, sf_byte_b add
+// another).
+__device__ __forceinline__ uint32_t idesc_mx8(int m, int n, bool b_mn = false) {
+  return (b_mn ? (1u << 16) : 0u) | (static_cast<uint32_t>(n >> 3) << 17) | (1u << 23) |
+         (static_cast<uint32_t>(m >> 4) << 24);
+}
+__device__ __forceinline__ uint32_t sf_byte_a(int i) { return static_cast<uint32_t>(i) << 29; }
+__device__ __forceinline__ uint32_t sf_byte_b(int i) { return static_cast<uint32_t>(i) << 4; }
+// 32 rows of 16 bytes in shared memory -> 4 TMEM columns of every lane quarter: row r's
+// word j is the scale word of operand row 32 j + r.
+__device__ __forceinline__ void tc_copy_scales(uint32_t tmem, uint32_t saddr, uint32_t on) {
+  uint64_t d = static_cast<uint64_t>((saddr & 0x3FFFFu) >> 4);
+  d |= static_cast<uint64_t>(128 >> 4) << 32;   // 8 rows of 16 bytes follow each other
+  d |= static_cast<uint64_t>(1) << 46;
+  asm volatile(
+      "{\n\t.reg .pred q;\n\t"
+      "setp.ne.b32 q, %2, 0;\n\t"
+      "@q tcgen05.cp.cta_group::1.32x128b.warpx4 [%0], %1;\n\t}" ::"r"(tmem),
+      "l"(d), "r"(on)
+      : "memory");
+}
+
 // 32 consecutive TMEM columns of this warp's 32 lanes -> v[0..31] (one lane each).
 __device__ __forceinline__ void tmem_ld32(uint32_t taddr, float (&v)[32]) {
   uint32_t r[32];
