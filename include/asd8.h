@@ -77,7 +77,8 @@ asd_status asd8_kv_quantize(const asd_dims* dims, const void* k_cache, const voi
  * What is rounded, beside the output: a softmax weight by 2^-8 of it or, in the context, by
  * 2^-16 of the largest product of a weight and a V scale among the 32 positions [32 i, 32 i +
  * 32) it is in, where that is more.  So neither tokens far below the row's largest weight
- * nor blocks of V far below the largest lose what they add.
+ * nor blocks of V far below the largest lose what they add.  Components of q below 2^-13
+ * of their row's largest are rounded by up to 2^-20 of that one (in the context's scores).
  * With one node per sequence (max_nodes 1, parent -1) it is the attention of a plain
  * decode step.
  */

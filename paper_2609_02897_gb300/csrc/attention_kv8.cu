@@ -2,10 +2,11 @@
 // cores, without turning the cache into a wider type: its e4m3 bytes go from TMA to
 // shared memory and are operands as they are.
 //
-//   S = q . K      q = 2^eq (q1 + q2), two e4m3 terms of 4 significant bits each, which
-//                  hold a bf16 number's 8 exactly (elements below 2^-10 of the row's
-//                  largest to 2^-18 of that one); S = q1 K^T + q2 K^T, two MMAs of half a
-//                  bf16 MMA's time, products exact, fp32 sums
+//   S = q . K      q = 2^eq (q1 + q2), q1 in e4m3 (4 significant bits, to nearest) and q2, what
+//                  that leaves, in e5m2: its 3 bits hold the rest of a bf16 number's 8, and
+//                  its exponents reach as far as the number is at least 2^-13 of the row's
+//                  largest (smaller ones to 2^-20 of that one); S = q1 K^T + q2 K^T, two MMAs
+//                  of half a bf16 MMA's time, products exact, fp32 sums
 //   x_j            = S_j log2(e)/sqrt(D) 2^(eq + ek[block of j]): the block scales of K
 //                  are factors of the exponent
 //   P_j            = 2^(x_j + ev[block of j] - G + 7), ev the exponents of V's blocks, G the
@@ -115,9 +116,10 @@ __device__ __forceinline__ int swz8(int r, int c) {
   return r * D + ((D == 128 ? c ^ (r & 7) : c ^ ((r >> 1) & 3)) << 4);
 }
 
-// kind::f8f6f4 instruction descriptor: e4m3 x e4m3 -> fp32, both K-major.
-__device__ __forceinline__ uint32_t idesc_f8(int m, int n) {
-  return (1u << 4) | (static_cast<uint32_t>(n >> 3) << 17) | (static_cast<uint32_t>(m >> 4) << 24);
+// kind::f8f6f4 instruction descriptor: A e4m3 or e5m2, B e4m3 -> fp32, both K-major.
+__device__ __forceinline__ uint32_t idesc_f8(int m, int n, bool a_e5m2) {
+  return (1u << 4) | (a_e5m2 ? (1u << 7) : 0u) | (static_cast<uint32_t>(n >> 3) << 17) |
+         (static_cast<uint32_t>(m >> 4) << 24);
 }
 
 // MMAs that the issuing warp runs converged, with `on` set in one lane (tc.cuh).
@@ -305,6 +307,26 @@ __device__ __forceinline__ void two_terms(const float (&w)[4], uint32_t& hi, uin
       "mov.b32 %1, {c, d};\n\t}"
       : "=r"(hi), "=r"(lo)
       : "f"(w[0]), "f"(w[1]), "f"(w[2]), "f"(w[3]));
+}
+
+// Four values of at most 448 with 8 significant bits -> words of e4m3 and of what that leaves,
+// in e5m2.  (A value is exact in fp16, and so is the rest.)
+__device__ __forceinline__ void two_terms_wide(const float (&q)[4], uint32_t& hi, uint32_t& lo) {
+  asm("{\n\t.reg .b16 a, b, c, d;\n\t.reg .b32 p, q, r, s;\n\t"
+      "cvt.rn.f16x2.f32 p, %3, %2;\n\t"
+      "cvt.rn.f16x2.f32 q, %5, %4;\n\t"
+      "cvt.rn.satfinite.e4m3x2.f16x2 a, p;\n\t"
+      "cvt.rn.satfinite.e4m3x2.f16x2 b, q;\n\t"
+      "mov.b32 %0, {a, b};\n\t"
+      "cvt.rn.f16x2.e4m3x2 r, a;\n\t"
+      "cvt.rn.f16x2.e4m3x2 s, b;\n\t"
+      "sub.rn.f16x2 r, p, r;\n\t"
+      "sub.rn.f16x2 s, q, s;\n\t"
+      "cvt.rn.satfinite.e5m2x2.f16x2 c, r;\n\t"
+      "cvt.rn.satfinite.e5m2x2.f16x2 d, s;\n\t"
+      "mov.b32 %1, {c, d};\n\t}"
+      : "=r"(hi), "=r"(lo)
+      : "f"(q[0]), "f"(q[1]), "f"(q[2]), "f"(q[3]));
 }
 
 // bf16 pairs: a word with every value that is not finite as 0.
@@ -678,7 +700,7 @@ __device__ __forceinline__ bool softmax_role8(const Attn8Params& p8, const Item&
   const bool mine = r < it.nrows;
   const bool busy = (((warp & 3) * 32) & (span - 1)) < it.nrows;
 
-  // This half of the row's query: a bf16 copy, and two e4m3 terms under the row's scale.
+  // This half of the row's query: a bf16 copy, and two 8-bit terms under the row's scale.
   float c_row = p.scale_log2;
   {
     const uint4* qg = reinterpret_cast<const uint4*>(static_cast<const __nv_bfloat16*>(p.q) +
@@ -719,7 +741,7 @@ __device__ __forceinline__ bool softmax_role8(const Attn8Params& p8, const Item&
       for (int i = 0; i < 4; ++i) {
         const float2 x = bf16x2_f32(w[2 * i]), y = bf16x2_f32(w[2 * i + 1]);
         const float q[4] = {x.x * inv, x.y * inv, y.x * inv, y.y * inv};
-        two_terms(q, hi[i], lo[i]);
+        two_terms_wide(q, hi[i], lo[i]);
       }
       const int at = swz8<D>(row, (cq * (D / 8 / kSplit) + k) / 2);
       *reinterpret_cast<uint4*>(gbase + at) = make_uint4(hi[0], hi[1], hi[2], hi[3]);
@@ -1025,7 +1047,8 @@ __global__ void __launch_bounds__(kThreads8, 1)
     const uint32_t on = lane == 0 ? 1u : 0u;
     const uint32_t tm = __shfl_sync(0xffffffffu, tmem, 0);
     if (warp == 1) {
-      const uint32_t idesc_s = idesc_f8(kRows, kKeys), idesc_t = idesc_bf16(kRows, kKeys);
+      const uint32_t idesc_s[2] = {idesc_f8(kRows, kKeys, false), idesc_f8(kRows, kKeys, true)};
+      const uint32_t idesc_t = idesc_bf16(kRows, kKeys);
       ok = wait_warp(&sh.q_ready, 0, budget);
       tc_fence_after();
       int copy = 0;          // of tile t, and the parity of its tiles before
@@ -1051,8 +1074,8 @@ __global__ void __launch_bounds__(kThreads8, 1)
 #pragma unroll
             for (int ks = 0; ks < D / 32; ++ks) {
               const uint64_t a = desc8<D>(base + term * G::kQ8 + 32 * ks), k = desc8<D>(kst + 32 * ks);
-              if (cp.kHalves) mma_f8(sb, a, k, idesc_s, term + ks > 0 ? 1u : 0u, on);
-              else mma_f8_lanes(sb, a, k, idesc_s, skip, term + ks > 0 ? 1u : 0u, on);
+              if (cp.kHalves) mma_f8(sb, a, k, idesc_s[term], term + ks > 0 ? 1u : 0u, on);
+              else mma_f8_lanes(sb, a, k, idesc_s[term], skip, term + ks > 0 ? 1u : 0u, on);
             }
         } else {
 #pragma unroll

@@ -182,3 +182,16 @@ def test_weight_that_moves_along_the_context(layout, D):
             up = torch.linspace(-30, 30, 3000, device="cuda") * sign * math.sqrt(D) / 8.0
             call.k[call.first[b]:call.first[b] + 3000, :, 0] = up[:, None]
         call.check(range(len(nodes)), NEAR)
+
+
+@pytest.mark.parametrize("power", [6, 9, 12])
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("layout", LAYOUTS)
+def test_queries_with_one_large_component(layout, D, power):
+    """A component of q that is 2^6 to 2^12 times the others, where K is 0: the others give the
+    scores, and keep the bits that they have."""
+    nodes, Hq, Hkv = LAYOUTS[layout]
+    call = Call(power + D, nodes, [700] * len(nodes), Hq, Hkv, D, 16, spread=64.0)
+    call.q[..., 1:] /= 16.0                              # scores N(0, 4)
+    call.q[..., 0] = 2.0 ** (power - 4)
+    call.check(range(len(nodes)), NEAR)
