@@ -872,6 +872,34 @@ __device__ __forceinline__ bool softmax_role8(const Attn8Params& p8, const Item&
   return true;
 }
 
+// Key j of sequence b's context, KV head g, for items_past_grid.
+static_assert(kSoftmax8 == kSoftmaxThreads, "the softmax warps take the items past the grid");
+template <int D>
+struct Context8 {
+  const Attn8Params& p8;
+  __device__ __forceinline__ bool operator()(int b, int g, int j, int lane, float (&k)[D / 32],
+                                             float (&v)[D / 32]) const {
+    const AttnParams& p = p8.a;
+    size_t at;
+    if (!context_row(p, b, g, j, at)) return false;
+    // the row's scale block: a page's rows, or a sequence's, are p8.blocks of them
+    const int slots = p.page_size ? p.page_size : p.ctx_max;
+    const size_t block = at / slots * p8.blocks + at % slots / p8.block;
+    load(static_cast<const uint8_t*>(p.k_cache) + at * D, p8.k_exp[block], lane, k);
+    load(static_cast<const uint8_t*>(p.v_cache) + at * D, p8.v_exp[block], lane, v);
+    return true;
+  }
+  __device__ __forceinline__ static void load(const uint8_t* row, int byte, int lane, float (&x)[D / 32]) {
+    const float f = pow2(min(max(byte - kExpBias, kMinExp), 126));
+#pragma unroll
+    for (int k = 0; k < D / 32; k += 2) {
+      const float2 y = e4m3x2_f32(*reinterpret_cast<const uint16_t*>(row + lane * (D / 32) + k));
+      x[k] = y.x * f;
+      x[k + 1] = y.y * f;
+    }
+  }
+};
+
 // The item's values by shuffles, which makes them uniform to the compiler: with the warp's index
 // alike, loops and branches on them need no reconvergence and what they steer stays in uniform
 // registers (32 adaptive trees 78 -> 69 us, 8 x 64 nodes at context 16384 167 -> 156).
@@ -1175,6 +1203,8 @@ __global__ void __launch_bounds__(kThreads8, 1)
     }
   }
   if (warp == 2) tmem_dealloc(tmem, kTmemCols);
+  if (s_plan.past > 0 && warp >= kSoftmaxWarp)
+    items_past_grid<D>(p, s_plan, threadIdx.x - 32 * kSoftmaxWarp, Context8<D>{p8});
   pdl_wait();   // the next kernel's wait covers every earlier kernel
 }
 

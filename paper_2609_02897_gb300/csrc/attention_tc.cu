@@ -115,82 +115,19 @@ __device__ __forceinline__ bool attention_takes_pairs(const AttnParams& p) {
   return pairs <= p.nsm && static_cast<float>(longest) <= p.pair_ratio * one + 3.f;
 }
 
-// One-tile form: the items past the grid, which has a CTA for every item of
-// sequences that do not overlap.  A batch whose cu_nodes run backwards (reported as
-// ASD_ERR_TREE) can make more, and its well-formed sequences keep their outputs.
-// Plain loops over the keys, a warp per query row, by the eight softmax warps (tid:
-// thread among them) of every CTA when it is done.  (In the ping-pong form the
-// branch cost the tile loop 2 %; its grid covers every item instead.)
+// Key j of sequence b's context, KV head g, for items_past_grid.
 template <int D>
-__device__ __forceinline__ void items_past_grid(const AttnParams& p, PlanSmem& s, int tid) {
-  constexpr int kV = D / 32;   // a lane's columns
-  const int lane = tid & 31;
-  const __nv_bfloat16* kc = static_cast<const __nv_bfloat16*>(p.k_cache);
-  const __nv_bfloat16* vc = static_cast<const __nv_bfloat16*>(p.v_cache);
-  for (int idx = gridDim.x + blockIdx.x; idx < s.past; idx += gridDim.x) {
-    softmax_sync();   // everyone is done with the last item's sequence
-    for (int q = tid; q < p.B; q += kSoftmaxThreads) {
-      int first = 0;
-      for (int j = 0; j < p.B; ++j) first += s.order[j].x > s.order[q].x ? s.order[j].y : 0;
-      if (idx < first || idx >= first + s.order[q].y) continue;
-      s.seq = q;
-      s.first = first;
-      if (idx == first && p.part_cap > 0) p.plan[q] = make_int2(0, 1);   // nothing to merge
-    }
-    softmax_sync();
-    const int b = s.seq, s0 = s.s0[b], R = s.n[b] * p.G, rb = (R + kRows - 1) / kRows;
-    const int g = (idx - s.first) / rb, r0 = (idx - s.first - g * rb) * kRows;
-    for (int r = r0 + (tid >> 5); r < min(r0 + kRows, R); r += kSoftmaxThreads / 32) {
-      const int node = r / p.G;
-      const size_t row = static_cast<size_t>(s0 + node) * p.Hq + g * p.G + (r - node * p.G);
-      const __nv_bfloat16* qr = static_cast<const __nv_bfloat16*>(p.q) + row * D;
-      __nv_bfloat16* out = static_cast<__nv_bfloat16*>(p.out) + row * D;
-      float q[kV], o[kV], m = -INFINITY, l = 0.f;
-#pragma unroll
-      for (int k = 0; k < kV; ++k) {
-        q[k] = __bfloat162float(qr[lane * kV + k]) * p.scale_log2;
-        o[k] = 0.f;
-      }
-      auto key = [&](const __nv_bfloat16* kr, const __nv_bfloat16* vr) {
-        float x = 0.f;
-#pragma unroll
-        for (int k = 0; k < kV; ++k) x = fmaf(q[k], __bfloat162float(kr[lane * kV + k]), x);
-#pragma unroll
-        for (int off = 16; off > 0; off >>= 1) x += __shfl_xor_sync(0xffffffffu, x, off);
-        const float mn = fmaxf(m, x);
-        const float al = m == -INFINITY ? 0.f : exp2f(m - mn);
-        const float pe = x == -INFINITY ? 0.f : exp2f(x - mn);
-        l = l * al + pe;
-#pragma unroll
-        for (int k = 0; k < kV; ++k) o[k] = fmaf(pe, __bfloat162float(vr[lane * kV + k]), o[k] * al);
-        m = mn;
-      };
-      for (int j = 0; j < s.ctx[b]; ++j) {
-        size_t at = (static_cast<size_t>(b) * p.Hkv + g) * p.ctx_max + j;
-        if (p.page_size) {
-          const int page = p.page_table[static_cast<size_t>(b) * p.pages_per_seq + j / p.page_size];
-          if (page < 0 || page >= p.num_pages) {
-            set_status(p.status, ASD_ERR_CTX_RANGE);
-            continue;
-          }
-          at = (static_cast<size_t>(page) * p.Hkv + g) * p.page_size + j % p.page_size;
-        }
-        key(kc + at * D, vc + at * D);
-      }
-      for (int u = node; u >= 0;) {   // the node and its ancestors
-        const size_t at = (static_cast<size_t>(s0 + u) * p.Hkv + g) * D;
-        key(static_cast<const __nv_bfloat16*>(p.tree_k) + at,
-            static_cast<const __nv_bfloat16*>(p.tree_v) + at);
-        const int pu = p.parent[s0 + u];
-        u = pu < u ? pu : -1;
-      }
-      const float inv = l > 0.f ? 1.f / l : 0.f;
-#pragma unroll
-      for (int k = 0; k < kV; ++k)
-        out[lane * kV + k] = __float2bfloat16_rn(o[k] * inv);
-    }
+struct BfContext {
+  const AttnParams& p;
+  __device__ __forceinline__ bool operator()(int b, int g, int j, int lane, float (&k)[D / 32],
+                                             float (&v)[D / 32]) const {
+    size_t at;
+    if (!context_row(p, b, g, j, at)) return false;
+    load_columns(static_cast<const __nv_bfloat16*>(p.k_cache) + at * D, lane, k);
+    load_columns(static_cast<const __nv_bfloat16*>(p.v_cache) + at * D, lane, v);
+    return true;
   }
-}
+};
 
 // Issues one K (which = 0) or V (which = 1) tile t into `dst` (producer lane 0;
 // contiguous cache or tree keys).
@@ -815,7 +752,7 @@ __global__ void __launch_bounds__(kThreads, 1)
   tc_fence_after();
   if (warp == 10) tmem_dealloc(tmem, kTmemCols);
   if (s_plan.past > 0 && warp >= 2 && warp < 10)
-    items_past_grid<D>(p, s_plan, threadIdx.x - 64);
+    items_past_grid<D>(p, s_plan, threadIdx.x - 64, BfContext<D>{p});
   pdl_wait();   // the next kernel's wait covers every earlier kernel
 }
 

@@ -336,5 +336,95 @@ __device__ __forceinline__ void tree_masks(const AttnParams& p, const Item& it, 
   softmax_sync<N>();
 }
 
+// Cache row of context position j of sequence b, KV head g; false (and reported) when its page
+// id is outside the pool.
+__device__ __forceinline__ bool context_row(const AttnParams& p, int b, int g, int j, size_t& at) {
+  if (p.page_size == 0) {
+    at = (static_cast<size_t>(b) * p.Hkv + g) * p.ctx_max + j;
+    return true;
+  }
+  const int page = p.page_table[static_cast<size_t>(b) * p.pages_per_seq + j / p.page_size];
+  if (page < 0 || page >= p.num_pages) {
+    set_status(p.status, ASD_ERR_CTX_RANGE);
+    return false;
+  }
+  at = (static_cast<size_t>(page) * p.Hkv + g) * p.page_size + j % p.page_size;
+  return true;
+}
+
+// A lane's columns of a row of D = 32 V bf16 values.
+template <int V>
+__device__ __forceinline__ void load_columns(const __nv_bfloat16* row, int lane, float (&x)[V]) {
+#pragma unroll
+  for (int k = 0; k < V; ++k) x[k] = __bfloat162float(row[lane * V + k]);
+}
+
+// One-tile form: the items past the grid, which has a CTA for every item of
+// sequences that do not overlap.  A batch whose cu_nodes run backwards (reported as
+// ASD_ERR_TREE) can make more, and its well-formed sequences keep their outputs.
+// Plain loops over the keys, a warp per query row, by the eight softmax warps (tid:
+// thread among them) of every CTA when it is done; `context` gives a lane's columns of
+// a context position's K and V.  (In the ping-pong form the branch cost the tile loop
+// 2 %; its grid covers every item instead.)
+template <int D, typename Context>
+__device__ __forceinline__ void items_past_grid(const AttnParams& p, PlanSmem& s, int tid,
+                                                const Context& context) {
+  constexpr int kV = D / 32;   // a lane's columns
+  const int lane = tid & 31;
+  for (int idx = gridDim.x + blockIdx.x; idx < s.past; idx += gridDim.x) {
+    softmax_sync();   // everyone is done with the last item's sequence
+    for (int q = tid; q < p.B; q += kSoftmaxThreads) {
+      int first = 0;
+      for (int j = 0; j < p.B; ++j) first += s.order[j].x > s.order[q].x ? s.order[j].y : 0;
+      if (idx < first || idx >= first + s.order[q].y) continue;
+      s.seq = q;
+      s.first = first;
+      if (idx == first && p.part_cap > 0) p.plan[q] = make_int2(0, 1);   // nothing to merge
+    }
+    softmax_sync();
+    const int b = s.seq, s0 = s.s0[b], R = s.n[b] * p.G, rb = (R + kRows - 1) / kRows;
+    const int g = (idx - s.first) / rb, r0 = (idx - s.first - g * rb) * kRows;
+    for (int r = r0 + (tid >> 5); r < min(r0 + kRows, R); r += kSoftmaxThreads / 32) {
+      const int node = r / p.G;
+      const size_t row = static_cast<size_t>(s0 + node) * p.Hq + g * p.G + (r - node * p.G);
+      float q[kV], o[kV], kx[kV], vx[kV], m = -INFINITY, l = 0.f;
+      load_columns(static_cast<const __nv_bfloat16*>(p.q) + row * D, lane, q);
+#pragma unroll
+      for (int k = 0; k < kV; ++k) {
+        q[k] *= p.scale_log2;
+        o[k] = 0.f;
+      }
+      auto key = [&] {
+        float x = 0.f;
+#pragma unroll
+        for (int k = 0; k < kV; ++k) x = fmaf(q[k], kx[k], x);
+#pragma unroll
+        for (int off = 16; off > 0; off >>= 1) x += __shfl_xor_sync(0xffffffffu, x, off);
+        const float mn = fmaxf(m, x);
+        const float al = m == -INFINITY ? 0.f : exp2f(m - mn);
+        const float pe = x == -INFINITY ? 0.f : exp2f(x - mn);
+        l = l * al + pe;
+#pragma unroll
+        for (int k = 0; k < kV; ++k) o[k] = fmaf(pe, vx[k], o[k] * al);
+        m = mn;
+      };
+      for (int j = 0; j < s.ctx[b]; ++j)
+        if (context(b, g, j, lane, kx, vx)) key();
+      for (int u = node; u >= 0;) {   // the node and its ancestors
+        const size_t at = (static_cast<size_t>(s0 + u) * p.Hkv + g) * D;
+        load_columns(static_cast<const __nv_bfloat16*>(p.tree_k) + at, lane, kx);
+        load_columns(static_cast<const __nv_bfloat16*>(p.tree_v) + at, lane, vx);
+        key();
+        const int pu = p.parent[s0 + u];
+        u = pu < u ? pu : -1;
+      }
+      const float inv = l > 0.f ? 1.f / l : 0.f;
+      __nv_bfloat16* out = static_cast<__nv_bfloat16*>(p.out) + row * D;
+#pragma unroll
+      for (int k = 0; k < kV; ++k) out[lane * kV + k] = __float2bfloat16_rn(o[k] * inv);
+    }
+  }
+}
+
 }  // namespace
 }  // namespace asd
