@@ -22,7 +22,7 @@ struct Kv8Params {
   const int32_t* path_len;
   int32_t* ctx_len_out;
   int* status;
-  int in_step;                // compact: behind a step's tail, which checked the path
+  int in_step;                // compact: behind a step's tail, whose call's status word it adds to
   int clear_status;           // set by the launch: the grid is one cluster, whose first CTA
                               // clears the status word
   int B, T, Hkv, D, ctx_max, page_size, pages_per_seq, num_pages, block, max_nodes, max_path;

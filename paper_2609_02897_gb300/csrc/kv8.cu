@@ -160,8 +160,7 @@ __global__ void __launch_bounds__(kCommitThreads) kv8_compact_kernel(const Kv8Pa
   if (threadIdx.x == 0) {
     if (!tree_ok) set_status(p.status, ASD_ERR_TREE);
     else if (!path_ok) set_status(p.status, ASD_ERR_SHAPE);
-    // (behind a step, whose tree preparation reports it, path_len is 0 then)
-    else if (!ctx_ok && !p.in_step) set_status(p.status, ASD_ERR_CTX_RANGE);
+    else if (!ctx_ok) set_status(p.status, ASD_ERR_CTX_RANGE);
     p.ctx_len_out[b] = ctx + len;
   }
   if (len == 0) return;
