@@ -133,7 +133,8 @@ __device__ __forceinline__ uint32_t rescale4(uint32_t w, float f) {
   return e4m3x2(a.x, a.y, f) | (e4m3x2(b.x, b.y, f) << 16);
 }
 
-// One CTA per sequence; the path is checked once, then every warp takes blocks.
+// One CTA per sequence; the path and the pages that it is written to are checked once, then
+// every warp takes blocks.
 template <int NC>
 __global__ void __launch_bounds__(kCommitThreads) kv8_compact_kernel(const Kv8Params p) {
   __shared__ int s_path[kMaxNodes];
@@ -155,7 +156,18 @@ __global__ void __launch_bounds__(kCommitThreads) kv8_compact_kernel(const Kv8Pa
     }
   __syncthreads();
   const bool path_ok = len_ok && !s_bad;
-  const bool ctx_ok = ctx >= 0 && path_ok && ctx <= p.ctx_max - len;
+  bool ctx_ok = ctx >= 0 && path_ok && ctx <= p.ctx_max - len;
+  if (p.page_size) {   // nothing is written where one of the pages is outside the pool
+    bool bad = false;
+    if (ctx_ok && len > 0) {
+      const int first = ctx / p.page_size, last = (ctx + len - 1) / p.page_size;
+      for (int k = first + threadIdx.x; k <= last; k += kCommitThreads) {
+        const int page = p.page_table[static_cast<size_t>(b) * p.pages_per_seq + k];
+        bad = bad || page < 0 || page >= p.num_pages;
+      }
+    }
+    if (__syncthreads_or(bad)) ctx_ok = false;
+  }
   if (!ctx_ok) len = 0;
   if (threadIdx.x == 0) {
     if (!tree_ok) set_status(p.status, ASD_ERR_TREE);
@@ -170,10 +182,7 @@ __global__ void __launch_bounds__(kCommitThreads) kv8_compact_kernel(const Kv8Pa
     const bool is_v = i0 & 1;
     const int g = (i0 >> 1) % p.Hkv, j = j0 + (i0 >> 1) / p.Hkv;
     size_t row, scale;
-    if (!block_at(p, b, g, j, row, scale)) {
-      if (lane == 0) set_status(p.status, ASD_ERR_CTX_RANGE);
-      continue;
-    }
+    if (!block_at(p, b, g, j, row, scale)) continue;   // (no page: checked above)
     const int old = max(0, min(p.block, ctx - j * p.block));          // earlier rows of the block
     const int end = min(p.block, ctx + len - j * p.block);            // first row behind the path
     uint8_t* exps = (is_v ? p.v_exp : p.k_exp) + scale;
