@@ -294,7 +294,7 @@ struct TailParams {
   int32_t* path_len;
   int32_t* bonus;
   int32_t* n_promoted;
-  // compact
+  // compact; walk of a step: ctx_len (null otherwise) and page_table, where the path will go
   const void* tree_k;
   const void* tree_v;
   void* k_cache;

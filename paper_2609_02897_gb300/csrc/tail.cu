@@ -18,6 +18,10 @@
 //            3 greedy with a single promotion;
 //  compact   copy the path's tree K/V into cache slots ctx_len .. ctx_len +
 //            path_len - 1 (contiguous or through the page table).
+// A path whose slots do not exist (past the cache's end, or in a page outside the
+// pool) is dropped whole: walk, where it is given the context lengths, makes it a path of
+// no nodes, and nothing is copied.  Its page ids are loaded before the call's earlier
+// kernels are waited for.
 #include <climits>
 
 #include "kernels.h"
@@ -27,6 +31,7 @@ namespace {
 
 constexpr int kTailThreads = 1024;     // 32 warps: one node's merge per warp
 constexpr int kMaxTailCluster = 16;    // CTAs of a cluster (more than 8: not portable)
+constexpr int kTouched = kMaxNodes / 8 + 1;   // pages that a path may touch
 
 __global__ void __launch_bounds__(kTailThreads) tail_kernel(const TailParams p) {
   __shared__ int s_par[kMaxNodes];
@@ -42,6 +47,7 @@ __global__ void __launch_bounds__(kTailThreads) tail_kernel(const TailParams p) 
   __shared__ int s_bc1[kMaxNodes];                   // rule 1: best child, promotion left
   __shared__ float s_ratio[kMaxNodes];               // rules 2, 3
   __shared__ unsigned long long s_bp[kMaxNodes];     // rules 2, 3: best promoted child key
+  __shared__ int s_page[kTouched];   // from the context's end on; -1: outside the pool
   __shared__ int s_maxd, s_deep, s_len, s_skip;
 
   // Until pdl_wait() this kernel reads only caller inputs (cu_nodes, parent,
@@ -75,6 +81,19 @@ __global__ void __launch_bounds__(kTailThreads) tail_kernel(const TailParams p) 
     return;
   }
   const int n = e - s;
+  const int ctx = p.ctx_len ? p.ctx_len[b] : 0;
+  if (p.ctx_len && p.page_size && i < kTouched) {
+    const int k = max(ctx, 0) / p.page_size + i;
+    const int page = k < p.pages_per_seq ? p.page_table[static_cast<size_t>(b) * p.pages_per_seq + k] : -1;
+    s_page[i] = page < p.num_pages ? page : -1;
+  }
+  // whether slots ctx .. ctx + len - 1 exist
+  auto fits = [&](int len) {
+    bool ok = ctx >= 0 && ctx <= p.ctx_max - len;
+    if (ok && p.page_size && len > 0)
+      for (int k = 0; k <= (ctx % p.page_size + len - 1) / p.page_size; ++k) ok = ok && s_page[k] >= 0;
+    return ok;
+  };
 
   bool okn = true;
   if (i < n) {
@@ -238,6 +257,10 @@ __global__ void __launch_bounds__(kTailThreads) tail_kernel(const TailParams p) 
           set_status(p.status, ASD_ERR_SHAPE);
           len = 0;
         }
+        if (p.ctx_len && len > 0 && !fits(len)) {
+          set_status(p.status, ASD_ERR_CTX_RANGE);
+          len = 0;
+        }
         s_len = len;
         p.path_len[b] = len;
         p.bonus[b] = len > 0 ? s_arg[u] : -1;
@@ -265,8 +288,8 @@ __global__ void __launch_bounds__(kTailThreads) tail_kernel(const TailParams p) 
         if (u < 0 || u >= n) ok = false;
         else s_path[k] = u;
       }
-      if (!ok) {
-        set_status(p.status, ASD_ERR_SHAPE);
+      if (!ok || !fits(len)) {
+        set_status(p.status, ok ? ASD_ERR_CTX_RANGE : ASD_ERR_SHAPE);
         len = 0;
         s_skip = 1;
       }
@@ -277,11 +300,8 @@ __global__ void __launch_bounds__(kTailThreads) tail_kernel(const TailParams p) 
 
   // ------------------------------------------------------------------ commit
   if (p.mode & kTailCompact) {
-    const int ctx = p.ctx_len[b];
     const int len = s_len;
-    const bool ctx_ok = ctx >= 0 && ctx + len <= p.ctx_max;
-    if (i == 0 && !ctx_ok && !s_skip) set_status(p.status, ASD_ERR_CTX_RANGE);
-    if (s_skip || !ctx_ok) {
+    if (s_skip) {
       if (i == 0) p.ctx_len_out[b] = ctx;
       return;
     }
@@ -303,11 +323,7 @@ __global__ void __launch_bounds__(kTailThreads) tail_kernel(const TailParams p) 
       if (p.page_size == 0) {
         dst = ((static_cast<size_t>(b) * p.Hkv + g) * p.ctx_max + slot) * row_bytes + ch * 16;
       } else {
-        const int page = p.page_table[static_cast<size_t>(b) * p.pages_per_seq + slot / p.page_size];
-        if (page < 0 || page >= p.num_pages) {
-          set_status(p.status, ASD_ERR_CTX_RANGE);
-          continue;
-        }
+        const int page = s_page[slot / p.page_size - ctx / p.page_size];
         dst = ((static_cast<size_t>(page) * p.Hkv + g) * p.page_size + slot % p.page_size) *
                   row_bytes + ch * 16;
       }
