@@ -382,6 +382,8 @@ asd_status asd8_verify_step(const asd_dims* dims, const asd8_verify_args* args, 
   t.path_len = a->path_len;
   t.bonus = a->bonus;
   t.n_promoted = a->n_promoted;
+  t.ctx_len = a->ctx_len;   // (a path that does not fit is none)
+  t.page_table = a->page_table;
   if (launch_tail(t, c.st) != cudaSuccess) return ASD_ERR_CUDA;
   Kv8Params k = kv8_params(c, args->cache, a->tree_k, a->tree_v, a->page_table, a->ctx_len);
   k.cu_nodes = a->cu_nodes;

@@ -142,3 +142,15 @@ def test_commit_context_lengths_at_the_end_of_the_range():
                            t["page_table"], k, v, out, ws)
         assert asd.asd_get_device_status(ws) == 5
         assert torch.equal(out, lens) and torch.equal(k, before[0]) and torch.equal(v, before[1])
+
+
+@pytest.mark.parametrize("page,ctx", [(0, 1535), (16, 1535), (16, 80)])
+def test_step8_has_no_path_where_slots_are_missing(page, ctx):
+    case, dims, t, step, cache, _ = _setup(page=page, ctx=(500, ctx, 0, 1300), seed=page + ctx, tau=1e-20)
+    if ctx == 80:
+        t["page_table"][1, 5] = -7
+    out = step.run()
+    torch.cuda.synchronize()
+    assert step.device_status() == 5
+    _no_path(out, 1, ctx)
+    assert (out["path_len"][[0, 3]] > 1).all() and out["path_len"][2] == 1
