@@ -13,7 +13,7 @@ namespace {
 
 constexpr int kRows = kAttnTcRows;   // query rows per CTA = TMEM lanes
 constexpr int kKeys = kAttnTcKeys;   // keys per tile
-constexpr int kThreads = 384;   // twelve warps (the roles above; the ping-pong form's below)
+constexpr int kThreads = 384;   // twelve warps (each kernel names their roles)
 constexpr int kSoftmaxThreads = 256;   // eight warps: two per TMEM lane quarter
 
 // Named barrier 1 of the softmax warps (N threads).
