@@ -92,6 +92,7 @@ class Cache8:
     def values(self, which: str) -> torch.Tensor:
         """What the cache's bytes stand for: fp32 `k` or `v`."""
         q, e = (self.k, self.k_exp) if which == "k" else (self.v, self.v_exp)
+        e = e.view(torch.uint8)   # (whatever one-byte type they came in)
         scale = torch.ldexp(torch.ones_like(e, dtype=torch.float32), e.int() - EXP_BIAS)
         rows = q.shape[2]
         return q.view(torch.float8_e4m3fn).float() * scale.repeat_interleave(self.block, 2)[:, :, :rows, None]
