@@ -195,3 +195,16 @@ def test_queries_with_one_large_component(layout, D, power):
     call.q[..., 1:] /= 16.0                              # scores N(0, 4)
     call.q[..., 0] = 2.0 ** (power - 4)
     call.check(range(len(nodes)), NEAR)
+
+
+@pytest.mark.parametrize("context,tree", [(0.0, 80), (0.0, 120), (2.0 ** -70, 0), (2.0 ** 80, 0), (2.0 ** 110, 110)])
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("layout", LAYOUTS)
+def test_values_of_context_and_tree_far_apart(layout, D, context, tree):
+    """V of the context nothing or tiny beside the tree's, or the other way round, or both near
+    the largest numbers."""
+    nodes, Hq, Hkv = LAYOUTS[layout]
+    call = Call(D, nodes, [300] * len(nodes), Hq, Hkv, D, 16)
+    call.v *= context
+    call.tree_v *= 2.0 ** tree
+    call.check(range(len(nodes)), NEAR)
