@@ -38,7 +38,7 @@
 // More rows fill the tile, and the softmax is what takes the time.  The two threads of a lane
 // then have an O each, the P.V of the tile's first and second 64 keys, and neither waits for
 // the other within a tile; the output joins them as it does copies (8 x 64 nodes at context
-// 16384 175 -> 168 us).
+// 16384 took 4 % less by it).
 //
 // TMEM (512 columns): with copies O [0, D), S [128, 256), P of copy k [256 + 64 k, 320 + 64 k),
 // scales [448, 512) with D = 128 (which leaves room for three copies), [64, 128) with D = 64.
@@ -58,10 +58,10 @@
 // measured copy rate; the tensor core 1080 (four terms of 128 x 128 x 128); shared memory
 // 1020 (TMA's writes 256, MMA operands 768); converting K and V to bf16 on the way would
 // take 1790 there.  Up to 64 rows that is near the copy rate once the tiles run (one token
-// at 8 x 16384 58 us, 4.6 TB/s over the whole call), and short contexts are bound by what
+// at 8 x 16384 59 us, 4.5 TB/s over the whole call), and short contexts are bound by what
 // stands around the tiles: plan, query terms, first copies, output and merge, 12 us (1 x
 // 1000 14 us, 8 nodes at 32k 26).  With 128 rows a tile takes 1800 cycles, of which the
-// softmax warps issue for 1000 (8 x 64 nodes on 128 of 152 SMs 147 us, 0.93 PFLOP/s, on scores
+// softmax warps issue for 1000 (8 x 64 nodes on 128 of 152 SMs 143 us, 0.96 PFLOP/s, on scores
 // as spread as a model's).
 #include <algorithm>
 
@@ -379,10 +379,10 @@ struct Copies {
   __device__ __forceinline__ explicit Copies(int nrows)
       : own(__all_sync(0xffffffffu, nrows <= 32) ? kMost : (__all_sync(0xffffffffu, nrows <= 64) ? 2 : 1)) {}
   __device__ __forceinline__ int rep() const { return REP == 0 ? own : (REP == kManyCopies ? kMost : REP); }
-  __device__ __forceinline__ int span() const {   // TMEM lanes of a copy
-    return rep() > 2 ? kRows / 4 : kRows / rep();
-  }
-  __device__ __forceinline__ int warps() const { return span() / 32 * kSplit; }   // softmax, of a copy
+  // TMEM lane quarters of a copy (log2), and lanes
+  __device__ __forceinline__ int quarters_log() const { return rep() > 2 ? 0 : 2 - (rep() >> 1); }
+  __device__ __forceinline__ int span() const { return 32 << quarters_log(); }
+  __device__ __forceinline__ int warps() const { return kSplit << quarters_log(); }   // softmax, of a copy
   // Each key half has an O of its own, the second at column D; P then takes the place of S,
   // in kOverBufs buffers.
   static constexpr bool kHalves = REP == 1;
@@ -391,12 +391,15 @@ struct Copies {
   __device__ __forceinline__ uint32_t s_col(int t) const {
     return kHalves ? 2 * D + 128 * (t % kOverBufs) : 128;
   }
-  __device__ __forceinline__ uint32_t p_col(int t) const {
-    return kHalves ? s_col(t) : 256 + 64 * (t % p_bufs());
+  // The buffer of tile t's P, which is copy `copy`'s (t modulo their number; a division that
+  // is not by a constant would stand in every tile's chain).
+  __device__ __forceinline__ int p_buf(int t, int copy) const { return rep() == 1 ? t & 1 : copy; }
+  __device__ __forceinline__ uint32_t p_col(int t, int copy) const {
+    return kHalves ? s_col(t) : 256 + 64 * p_buf(t, copy);
   }
   // scale words of P and of V
-  __device__ __forceinline__ uint32_t sfa_col(int t) const {
-    return kHalves ? s_col(t) + kCols / 2 : sfb_col(t) + 4 + 4 * (t % p_bufs());
+  __device__ __forceinline__ uint32_t sfa_col(int t, int copy) const {
+    return kHalves ? s_col(t) + kCols / 2 : sfb_col(t) + 4 + 4 * p_buf(t, copy);
   }
   __device__ __forceinline__ uint32_t sfb_col(int t) const {
     return kHalves ? s_col(t) + kCols / 2 + 4 : (D == 64 ? 64 : 448);
@@ -586,7 +589,7 @@ struct Softmax {
         const bool rescale = t >= cp.rep() && __any_sync(0xffffffffu, need && had);
         const float alpha = need && had ? exp2f(R - top) : 1.f;
         if (need) R = top;
-        const uint32_t p_at = lane_base + cp.p_col(t) +
+        const uint32_t p_at = lane_base + cp.p_col(t, copy) +
                               cq * (HALVES ? kCols : tree ? kCols / 2 : kCols / 4);
         weights(x, mt, u, p_at, HALVES ? kCols / 4 : kCols / 2, sc, sh.sfa[t % kRing], tree);
         if (rescale) {
@@ -617,7 +620,7 @@ struct Softmax {
         // t - 4, consumed: P.V of tile t - 4 is done.)
         if (!bad && wait_warp(&sh.v_full[t % kStages], (t / kStages) & 1, budget)) {
           // thread among those of the copy
-          const int per = cp.span() / 32, tid = (cq * per + (quarter & (per - 1))) * 32 + lane;
+          const int per = 1 << cp.quarters_log(), tid = (cq * per + (quarter & (per - 1))) * 32 + lane;
           const int of = kSplit * 32 * per;
           uint8_t* vt = gbase + G::kVOff + t % kStages * G::kTile;
           constexpr int kChunks = D / 16;
@@ -696,7 +699,7 @@ __device__ __forceinline__ bool softmax_role8(const Attn8Params& p8, const Item&
   const int tid = threadIdx.x - 32 * kSoftmaxWarp;
   const uint32_t lane_base = tmem + (static_cast<uint32_t>((warp & 3) * 32) << 16);
   const int span = cp.span();                  // rows of a copy
-  const int r = row & (span - 1), copy = row / span;
+  const int r = row & (span - 1), copy = row >> (5 + cp.quarters_log());
   const bool mine = r < it.nrows;
   const bool busy = (((warp & 3) * 32) & (span - 1)) < it.nrows;
 
@@ -755,7 +758,7 @@ __device__ __forceinline__ bool softmax_role8(const Attn8Params& p8, const Item&
     for (int k = 0; rep > 1 && k < rep; ++k)
       if (k != copy)
         for (int c = 0; c < 64 / kSplit; c += 16)
-          tmem_st16u(lane_base + cp.p_col(k) + (64 / kSplit) * cq + c, z);
+          tmem_st16u(lane_base + cp.p_col(k, k) + (64 / kSplit) * cq + c, z);
     tmem_wait_st();
     tc_fence_before();
     __syncwarp();
@@ -1095,7 +1098,7 @@ __global__ void __launch_bounds__(kThreads8, 1)
         // the copy's lanes only
         uint32_t skip[4];
 #pragma unroll
-        for (int k = 0; k < 4; ++k) skip[k] = 32 * k / cp.span() == copy ? 0u : 0xffffffffu;
+        for (int k = 0; k < 4; ++k) skip[k] = k >> cp.quarters_log() == copy ? 0u : 0xffffffffu;
         if (!tree) {
 #pragma unroll
           for (int term = 0; term < 2; ++term)
@@ -1127,7 +1130,8 @@ __global__ void __launch_bounds__(kThreads8, 1)
       tc_fence_after();
       const uint32_t idesc_o = idesc_mx8(kRows, D, true), idesc_t = idesc_bf16(kRows, D, true);
       if (!cp.kHalves) tc_copy_scales(tm + cp.sfb_col(0), smem_u32(sh.sfb), on);
-      for (int j = 0; ok && j < it.ntiles; ++j) {
+      int copy = 0;   // of tile j
+      for (int j = 0; ok && j < it.ntiles; ++j, copy = copy + 1 == cp.rep() ? 0 : copy + 1) {
         const bool tree = j >= it.nctx;
         const int stage = j % kStages, b = j % kRing;
         ok = wait_warp(&sh.p_full[b], (j / kRing) & 1, budget) &&
@@ -1140,12 +1144,12 @@ __global__ void __launch_bounds__(kThreads8, 1)
         tc_fence_after();
         const uint32_t vst = base + (tree ? G::kTreeVOff : G::kVOff + stage * G::kTile);
         // P's columns of MMA step kk: in a row, or behind the start of either key half's S
-        const uint32_t pb = tm + cp.p_col(j);
+        const uint32_t pb = tm + cp.p_col(j, copy);
         const uint32_t half = cp.kHalves ? 1u : 0u, o1 = half * D;
         const uint32_t lo = half ? kCols / 4 : kCols / 2;
         if (!tree) {
           const uint32_t skip = half * (kCols - kCols / 4);
-          const uint32_t sfa = tm + cp.sfa_col(j), sfb = tm + cp.sfb_col(j);
+          const uint32_t sfa = tm + cp.sfa_col(j, copy), sfb = tm + cp.sfb_col(j);
           tc_copy_scales(sfa, smem_u32(sh.sfa[b]), on);
           if (half) tc_copy_scales(sfb, smem_u32(sh.sfb), on);
 #pragma unroll
@@ -1211,12 +1215,14 @@ __global__ void __launch_bounds__(kThreads8, 1)
 using Kernel = void(const CUtensorMap, const CUtensorMap, const CUtensorMap, const CUtensorMap,
                     const Attn8Params);
 
-// By the largest sequence's rows of a KV head (the items' then are no more): at most 32 fit four
-// copies, at most 64 two.  8 sequences at context 16384, four heads to a KV head, one / 8 / 16
-// nodes: four copies 58 / 65 / - us, two 66 / 71 / 73, none 85 / 89 / 91.  Where most sequences
-// have fewer rows than the largest, the items' own number: 8 nodes 68, 16 nodes 77.  Otherwise
-// one copy, an O for each key half, whatever an item's rows: ragged trees of 64 columns 46 us
-// (items' own number 50), 8 x 64 nodes at 16384 147 (170).
+// By the largest sequence's rows of a KV head (the items' then are no more): at most 32 fit three
+// or four copies, at most 64 two.  8 sequences at context 16384, four heads to a KV head, one / 8 /
+// 16 nodes: three copies 59 / 62 / - us, two 65 / 68 / 69, one - / - / 82.  Where sequences have
+// few rows on average beside a larger one, the items' own number: 32 of 2 to 24 nodes at contexts
+// 1000 to 8000 69 (one copy 79), 64 of 1 and 17 at 2000 83 (95).  (It costs a call whose time
+// the large ones set: 64 nodes beside 15 trees of 4 at 4000 56 (50).)  Otherwise one copy, an O
+// for each key half, whatever an item's rows: 16 trees of 16 to 96 nodes of 64 columns 51 (59),
+// 8 x 64 nodes at 16384 150 (173).
 template <int D, int BLK>
 Kernel* kernel_of_rows(int most, double mean) {
   return most <= 32   ? attn_kv8_kernel<D, BLK, kManyCopies>
