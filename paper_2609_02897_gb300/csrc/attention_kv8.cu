@@ -9,12 +9,12 @@
 //                  of half a bf16 MMA's time, products exact, fp32 sums
 //   x_j            = S_j log2(e)/sqrt(D) 2^(eq + ek[block of j]): the block scales of K
 //                  are factors of the exponent
-//   P_j            = 2^(x_j + ev[block of j] - G + 7), ev the exponents of V's blocks, G the
-//                  largest floor(x_j + ev) among the 32 keys that an MMA step takes: at most
-//                  2^8, again in two e4m3 terms (2^-8 of P, 2^-16 of the group's largest at
-//                  least)
-//   O += 2^(G-7-R) P V   two block-scaled MMAs over e4m3 V: the power of two is the MMA's scale
-//                  byte of the row and the group, so no weight is small in its own group, however
+//   P_j            = 2^(x_j + ev[block of j] - R - d + 7), ev the exponents of V's blocks, R a
+//                  reference of the row, d the largest floor(x_j + ev - R) among the 32 keys
+//                  that an MMA step takes: at most 2^8, again in two e4m3 terms (2^-8 of P,
+//                  2^-16 of the group's largest at least)
+//   O += 2^(d-7) P V   two block-scaled MMAs over e4m3 V: the power of two is the MMA's scale byte
+//                  of the row and the group, so no weight is small in its own group, however
 //                  far the group's lie below the row's largest or its V below the largest V;
 //                  output O 2^R / sum_j 2^x_j
 //
@@ -22,9 +22,13 @@
 // lay below half of that was lost to P.V and not to the sum: a token with 0.9 of the weight
 // in front of 16384 others cost them a quarter of what they add.)
 //
-// R, an integer per row, keeps O within fp32: it is moved, and O rescaled, when a group's G
-// exceeds it by more than kSlack, which scores of a model hardly ever do after their first
-// tile.
+// R is the largest x + ev of the row's first tile, and of a later one that exceeds it by more
+// than kSlack; O is rescaled then, behind the weights, and all rows of the warp that have a larger
+// one move at once.  The weight at R is a power of two, which P holds exactly: a token that
+// has most of a row's weight keeps it.  (On scores as spread as a model's, the listed cases' outputs
+// differ from fp32's by 8e-4 to 1.4e-3 of their norm, two bf16 roundings' flips included;
+// 1.5e-3 to 2.2e-3 with whole numbers for R.  kSlack = 5 gives 5e-4 to 1e-3 and costs 8 x 64
+// nodes at context 16384 3 %, 32 gives 9e-4 to 1.7e-3 and saves 1 %.)
 //
 // The last key tile holds the tree's own K and V in bf16: S and P.V of that tile are
 // kind::f16 MMAs on a bf16 copy of q and on P = 2^(x - R) <= 2 in bf16 (2^-8 of each weight).
@@ -81,7 +85,7 @@ constexpr int kThreads8 = 128 + kSoftmax8;
 constexpr int kRing = 4;          // barriers of S, P and P.V, in turn
 constexpr int kGroup = 32;        // keys of an MMA step, under one scale byte of a row
 constexpr float kTop = 7.f;       // a group's largest weight is held in [2^7, 2^8]
-constexpr float kSlack = 32.f;    // R is moved when a group's G exceeds it by more
+constexpr float kSlack = 8.f;     // R is moved when a group's largest x + ev exceeds it by more
 
 // Dynamic shared memory, 1024-byte aligned: q1, q2 [128 rows][D bytes], q in bf16
 // [D/64][128 rows][128 bytes], the K ring, the V ring.  The tree's bf16 K and V tiles
@@ -479,12 +483,11 @@ struct Softmax {
 #pragma unroll
       for (int h = 0; h < kCols / kGroup; ++h) {
         uint32_t hi[8], lo[8];
-        // (finite where the group has no key)
-        const float top = fmaxf(floorf(u[h]), -1e6f) - kTop;
-        // 2^(top - R), as little as a scale byte holds where it is less
-        const float b = fminf(fmaxf(top - rz + 127.f, 0.f), 254.f);
-        bytes |= static_cast<uint32_t>(b) << (8 * h);
-        const float to_sum = ex2_approx(top - mz);
+        // powers of two from R to the group's largest (finite where it has no key); the MMA's
+        // scale, as little as a byte holds where it is less
+        const float d = fmaxf(floorf(u[h] - rz), -1e6f) - kTop;
+        bytes |= static_cast<uint32_t>(fminf(fmaxf(d + 127.f, 0.f), 254.f)) << (8 * h);
+        const float top = rz + d, to_sum = ex2_approx(top - mz);
 #pragma unroll
         for (int g = 0; g < kGroup / BLK; ++g) {
           const int at = kGroup * h + BLK * g, sg = (cq * kCols + at) / 8;
@@ -570,7 +573,7 @@ struct Softmax {
         if (busy) {
           if (tree || valid < kKeys) mask(x, tree, valid);
           mt = maximum(x, sc, tree, u);
-          top = floorf(fmaxf(u[0], u[1]));
+          top = fmaxf(u[0], u[1]);
           if (!HALVES) sh.mx[e][cq][row] = top;
         }
       }
@@ -585,8 +588,12 @@ struct Softmax {
       if (!HALVES && t >= cp.p_bufs() && !wait_pv(t - cp.p_bufs())) bad = true;
       if (busy) {
         // (the tree's weights are not scaled: none above 2)
-        const bool had = R != -INFINITY, need = had ? top > R + (tree ? 0.f : kSlack) : top != -INFINITY;
+        const bool had = R != -INFINITY;
+        bool need = had ? top > R + (tree ? 0.f : kSlack) : top != -INFINITY;
         const bool rescale = t >= cp.rep() && __any_sync(0xffffffffu, need && had);
+        // where one of the warp's rows moves its reference all do: the next that has to is
+        // then many tiles away (the tree's tile, the last, keeps rows apart)
+        if (rescale && !tree) need = need || top > R;
         const float alpha = need && had ? exp2f(R - top) : 1.f;
         if (need) R = top;
         const uint32_t p_at = lane_base + cp.p_col(t, copy) +
