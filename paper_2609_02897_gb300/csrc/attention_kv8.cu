@@ -62,10 +62,10 @@
 // measured copy rate; the tensor core 1080 (four terms of 128 x 128 x 128); shared memory
 // 1020 (TMA's writes 256, MMA operands 768); converting K and V to bf16 on the way would
 // take 1790 there.  Up to 64 rows that is near the copy rate once the tiles run (one token
-// at 8 x 16384 59 us, 4.5 TB/s over the whole call), and short contexts are bound by what
+// at 8 x 16384 60 us, 4.5 TB/s over the whole call), and short contexts are bound by what
 // stands around the tiles: plan, query terms, first copies, output and merge, 12 us (1 x
 // 1000 14 us, 8 nodes at 32k 26).  With 128 rows a tile takes 1800 cycles, of which the
-// softmax warps issue for 1000 (8 x 64 nodes on 128 of 152 SMs 143 us, 0.96 PFLOP/s, on scores
+// softmax warps issue for 1000 (8 x 64 nodes on 128 of 152 SMs 147 us, 0.94 PFLOP/s, on scores
 // as spread as a model's).
 #include <algorithm>
 
@@ -1224,12 +1224,12 @@ using Kernel = void(const CUtensorMap, const CUtensorMap, const CUtensorMap, con
 
 // By the largest sequence's rows of a KV head (the items' then are no more): at most 32 fit three
 // or four copies, at most 64 two.  8 sequences at context 16384, four heads to a KV head, one / 8 /
-// 16 nodes: three copies 59 / 62 / - us, two 65 / 68 / 69, one - / - / 82.  Where sequences have
+// 16 nodes: three copies 60 / 63 / - us, two 67 / 69 / 71, one - / - / 83.  Where sequences have
 // few rows on average beside a larger one, the items' own number: 32 of 2 to 24 nodes at contexts
-// 1000 to 8000 69 (one copy 79), 64 of 1 and 17 at 2000 83 (95).  (It costs a call whose time
-// the large ones set: 64 nodes beside 15 trees of 4 at 4000 56 (50).)  Otherwise one copy, an O
-// for each key half, whatever an item's rows: 16 trees of 16 to 96 nodes of 64 columns 51 (59),
-// 8 x 64 nodes at 16384 150 (173).
+// 1000 to 8000 70 (one copy 82), 64 of 1 and 17 at 2000 84 (98).  (It costs a call whose time
+// the large ones set: 64 nodes beside 15 trees of 4 at 4000 58 (53).)  Otherwise one copy, an O
+// for each key half, whatever an item's rows: 16 trees of 16 to 96 nodes of 64 columns 51 (60),
+// 8 x 64 nodes at 16384, pages of 16, 152 (173).
 template <int D, int BLK>
 Kernel* kernel_of_rows(int most, double mean) {
   return most <= 32   ? attn_kv8_kernel<D, BLK, kManyCopies>
